@@ -318,6 +318,101 @@ lq_status logquant_decode_step_seq(const lq_config *cfg, lq_cache_seq *cache, co
 lq_status logquant_decode_plan_seq(const lq_config *cfg, const int32_t *n_fp, const int32_t *n_q,
                                    lq_plan *out);
 
+/* ---- 8-bit cache ---------------------------------------------------------------------
+ * A second kind of cache, for contexts whose every token is to stay (no filtering): keys
+ * and values are held as 8-bit floating-point codes with one scale for each block of
+ * `block` consecutive tokens of a kv head and tensor.  Half the bytes of a 16-bit cache,
+ * and one rounding to four significant bits whatever outlier channels a block has (an
+ * integer code of the block's largest element would leave the ordinary channels beside a
+ * ten times larger one 9 % of error; this leaves them 2.6 %).
+ *
+ * Quantizer of one block (G x d values x of type T): a = max |x|; scale s = 2^e with e the
+ * smallest integer >= -126 for which a <= 448 * 2^e; code = x / s (exact, s is a power of
+ * two) rounded to nearest even as e4m3 (OCP: 4 exponent and 3 mantissa bits, bias 7,
+ * largest 448, smallest 2^-9); value code * s (exact in T).  |x| is cut off at 1.875 * 2^15
+ * (fp16) or 1.875 * 2^127 (bf16) first, the largest value of T that the rounding cannot
+ * carry beyond T.  The newest tokens of a sequence, fewer than G, wait in T (its tail)
+ * until their block is full, so that what the cache holds depends on the tokens alone and
+ * not on the calls that brought them.  Finite inputs only.
+ *
+ * Layouts (bh, kperm as above, G = block, CAP = capacity):
+ *   k_codes  u8   index (((bh*(CAP/32) + t/32)*(d/32) + c/32)*64 + 16*((c%32)/8) + t%16)*16
+ *                       + 8*((t%32)/16) + c%8
+ *   v_codes  u8   index (((bh*(CAP/32) + t/32)*(d/32) + c/32)*64 + 16*(k/8) + c%16)*16
+ *                       + 8*((c%32)/16) + k%8,          k = kperm(t % 32)
+ *   k_scale, v_scale  f32  index bh*(CAP/G) + t/G
+ *   k_tail, v_tail    T    as k_fp, v_fp with CAP = G and t = position % G
+ * of the blocks that are full (n/G of them for a row of n tokens) and the n % G rows of
+ * the tail; other content is unspecified and never influences a result.
+ *
+ * Lengths are per batch row, as for lq_cache_seq: n is a HOST array of B entries, owned by
+ * the caller and updated by the calls; a row may be empty.  seq_state is DEVICE scratch
+ * (logquant_sizes8) through which calls hand the counts to their kernels; a cache serves
+ * one stream at a time.  DEVICE buffers that a call reads or writes start at a multiple of
+ * 16 bytes (else LQ_ERR_SHAPE).  Errors are detected before anything is launched or
+ * changed. */
+typedef struct {
+  int32_t B;           /* batch rows                                                   */
+  int32_t Hq;          /* query heads; query head h reads kv head h / (Hq/Hkv)         */
+  int32_t Hkv;         /* kv heads, Hq % Hkv == 0                                      */
+  int32_t d;           /* head dimension, one of 64, 96, 128                           */
+  int32_t block;       /* G: tokens that share a scale, 32/64/128                      */
+  int32_t dtype;       /* lq_dtype                                                     */
+  int32_t capacity;    /* max tokens per sequence, a multiple of `block`               */
+} lq_config8;
+
+typedef struct {
+  uint8_t  *k_codes, *v_codes;
+  float    *k_scale, *v_scale;
+  void     *k_tail, *v_tail;
+  int32_t  *n;           /* HOST [B]: tokens that row b holds, 0..capacity               */
+  void     *seq_state;   /* DEVICE scratch, lq_sizes8.seq_state bytes                    */
+} lq_cache8;
+
+/* Byte sizes (HOST out): codes, scale and tail are of one tensor (K or V). */
+typedef struct {
+  size_t codes, scale, tail, seq_state;
+  size_t workspace;      /* of logquant_decode_attn8 and logquant_decode_step8           */
+} lq_sizes8;
+lq_status logquant_sizes8(const lq_config8 *cfg, lq_sizes8 *out);
+
+/* Prepare a freshly allocated workspace (lq_sizes8.workspace bytes), as
+ * logquant_workspace_init does. */
+lq_status logquant_workspace_init8(const lq_config8 *cfg, void *workspace, void *stream);
+
+/* New tokens behind those that each row holds; blocks that become full are quantized in
+ * the same launch.
+ *   k_new, v_new : DEVICE [B][Hkv][n_max][d] T, row-major, of which row b's first n_new[b]
+ *   tokens are read; n_new : HOST array of B entries, 0 <= n_new[b] <= n_max (null: n_max
+ *   for every row).
+ * LQ_ERR_SHAPE for n_max < 1 or an n_new outside its range, LQ_ERR_CAPACITY if a row would
+ * pass `capacity`.  On success n[b] += n_new[b]. */
+lq_status logquant_append8(const lq_config8 *cfg, lq_cache8 *cache, const void *k_new,
+                           const void *v_new, const int32_t *n_new, int32_t n_max, void *stream);
+
+/* What the cache holds of tokens t0 .. t0+n-1, as values of T:
+ *   k_out, v_out : DEVICE [B][Hkv][n][d] T, row-major; either may be null (not wanted).
+ * Rows of the output at or behind a sequence's length are left as they were.
+ * Requires t0 >= 0, n >= 1, t0 + n <= capacity (else LQ_ERR_SHAPE). */
+lq_status logquant_read8(const lq_config8 *cfg, const lq_cache8 *cache, int32_t t0, int32_t n,
+                         void *k_out, void *v_out, void *stream);
+
+/* Decode attention over the 8-bit cache: out[b][h] = softmax_t(scale * q[b][h] . k_t)
+ * applied to v_t, t running over the tokens that row b holds, with the values that
+ * logquant_read8 gives (codes and scales are applied in registers); zeros for an empty row.
+ *   q, out, softmax_scale, workspace: as for logquant_decode_attn (sizes from
+ *   logquant_sizes8, prepared with logquant_workspace_init8). */
+lq_status logquant_decode_attn8(const lq_config8 *cfg, const lq_cache8 *cache, const void *q,
+                                float softmax_scale, void *out, void *workspace, void *stream);
+
+/* One decode step: logquant_append8 of one token for every row, then logquant_decode_attn8
+ * over the cache including it, with the results of the two calls.  One launch when no
+ * row's block becomes full, else two.
+ *   k_new, v_new : DEVICE [B][Hkv][1][d] T.  LQ_ERR_CAPACITY if a row is full. */
+lq_status logquant_decode_step8(const lq_config8 *cfg, lq_cache8 *cache, const void *k_new,
+                                const void *v_new, const void *q, float softmax_scale, void *out,
+                                void *workspace, void *stream);
+
 /* Measurement helper (not a step of the method): one streaming read of `bytes` bytes of
  * DEVICE memory at `buf` (16-byte aligned, bytes >= 16; a tail of bytes % 16 is not read),
  * enqueued on `stream`.  `sink`: DEVICE, 8192 uint32 words the kernel folds what it read

@@ -50,6 +50,19 @@ class lq_sizes(C.Structure):
                                           "v_meta", "pos_q", "workspace")]
 
 
+class lq_config8(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "block", "dtype", "capacity")]
+
+
+class lq_cache8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")] + [
+        ("n", C.POINTER(C.c_int32)), ("seq_state", C.c_void_p)]
+
+
+class lq_sizes8(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("codes", "scale", "tail", "seq_state", "workspace")]
+
+
 class lq_plan(C.Structure):
     _fields_ = [("blocks", C.c_int32), ("waves_per_block", C.c_int32), ("splits", C.c_int32),
                 ("fp_waves", C.c_int32), ("bytes_read", C.c_int64)]
@@ -60,6 +73,8 @@ EXPORTS = ("logquant_sizes", "logquant_workspace_bytes", "logquant_workspace_ini
            "logquant_decode_step", "logquant_decode_plan",
            "logquant_seq_state_bytes", "logquant_prefill_seq", "logquant_append_seq", "logquant_compress_seq",
            "logquant_decode_attn_seq", "logquant_decode_step_seq", "logquant_decode_plan_seq",
+           "logquant_sizes8", "logquant_workspace_init8", "logquant_append8", "logquant_read8",
+           "logquant_decode_attn8", "logquant_decode_step8",
            "logquant_read_probe", "logquant_status_string")
 
 if not os.path.exists(LIB_PATH):
@@ -114,6 +129,22 @@ _lib.logquant_decode_step_seq.argtypes = [C.POINTER(lq_config), C.POINTER(lq_cac
 _lib.logquant_decode_step_seq.restype = C.c_int
 _lib.logquant_decode_plan_seq.argtypes = [C.POINTER(lq_config), _I32P, _I32P, C.POINTER(lq_plan)]
 _lib.logquant_decode_plan_seq.restype = C.c_int
+_lib.logquant_sizes8.argtypes = [C.POINTER(lq_config8), C.POINTER(lq_sizes8)]
+_lib.logquant_sizes8.restype = C.c_int
+_lib.logquant_workspace_init8.argtypes = [C.POINTER(lq_config8), C.c_void_p, C.c_void_p]
+_lib.logquant_workspace_init8.restype = C.c_int
+_lib.logquant_append8.argtypes = [C.POINTER(lq_config8), C.POINTER(lq_cache8), C.c_void_p, C.c_void_p, _I32P, C.c_int32,
+                                  C.c_void_p]
+_lib.logquant_append8.restype = C.c_int
+_lib.logquant_read8.argtypes = [C.POINTER(lq_config8), C.POINTER(lq_cache8), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                C.c_void_p]
+_lib.logquant_read8.restype = C.c_int
+_lib.logquant_decode_attn8.argtypes = [C.POINTER(lq_config8), C.POINTER(lq_cache8), C.c_void_p, C.c_float, C.c_void_p,
+                                       C.c_void_p, C.c_void_p]
+_lib.logquant_decode_attn8.restype = C.c_int
+_lib.logquant_decode_step8.argtypes = [C.POINTER(lq_config8), C.POINTER(lq_cache8), C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.logquant_decode_step8.restype = C.c_int
 _lib.logquant_read_probe.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
 _lib.logquant_read_probe.restype = C.c_int
 _lib.logquant_status_string.argtypes = [C.c_int]
@@ -250,6 +281,35 @@ def logquant_read_probe(buf, nbytes, sink, stream=0):
     return _lib.logquant_read_probe(_ptr(buf), int(nbytes), _ptr(sink), stream)
 
 
+def logquant_sizes8(cfg):
+    out = lq_sizes8()
+    st = _lib.logquant_sizes8(_p(cfg), C.byref(out))
+    if st != LQ_OK:
+        raise LogQuantError(st, "logquant_sizes8")
+    return out
+
+
+def logquant_workspace_init8(cfg, workspace, stream=0):
+    return _lib.logquant_workspace_init8(_p(cfg), _ptr(workspace), stream)
+
+
+def logquant_append8(cfg, cache, k_new, v_new, n_new, n_max, stream=0):
+    return _lib.logquant_append8(_p(cfg), _p(cache), _ptr(k_new), _ptr(v_new), _i32(n_new), int(n_max), stream)
+
+
+def logquant_read8(cfg, cache, t0, n, k_out, v_out, stream=0):
+    return _lib.logquant_read8(_p(cfg), _p(cache), int(t0), int(n), _ptr(k_out), _ptr(v_out), stream)
+
+
+def logquant_decode_attn8(cfg, cache, q, softmax_scale, out, workspace, stream=0):
+    return _lib.logquant_decode_attn8(_p(cfg), _p(cache), _ptr(q), float(softmax_scale), _ptr(out), _ptr(workspace), stream)
+
+
+def logquant_decode_step8(cfg, cache, k_new, v_new, q, softmax_scale, out, workspace, stream=0):
+    return _lib.logquant_decode_step8(_p(cfg), _p(cache), _ptr(k_new), _ptr(v_new), _ptr(q), float(softmax_scale),
+                                      _ptr(out), _ptr(workspace), stream)
+
+
 def torch_dtype(dtype):
     import torch
     return torch.bfloat16 if dtype == "bf16" else torch.float16
@@ -265,6 +325,10 @@ def to_dev(x, dtype, device="cuda:0"):
 def make_config(B, Hq, Hkv, d, fp_budget, group, dtype, q_capacity, bits=2):
     return lq_config(B, Hq, Hkv, d, fp_budget, group, bits, LQ_BF16 if dtype == "bf16" else LQ_F16,
                      q_capacity)
+
+
+def make_config8(B, Hq, Hkv, d, block, dtype, capacity):
+    return lq_config8(B, Hq, Hkv, d, block, LQ_BF16 if dtype == "bf16" else LQ_F16, capacity)
 
 
 class DeviceCache:
@@ -434,3 +498,106 @@ class DeviceCacheSeq(DeviceCache):
     def view(self, b):
         """Counts of sequence b as a (cur, n_fp, n_q) triple."""
         return (self.cur[b], self.n_fp[b], self.n_q[b])
+
+
+class DeviceCache8:
+    """Owner of the device buffers of one lq_cache8 (torch tensors), its counts and the workspace.  Tensors are refused
+    (ValueError) unless they are of the cache's type, shape and device and contiguous.  A call goes to the current stream
+    of the cache's device, whichever device is current."""
+
+    BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")
+
+    def __init__(self, cfg, device="cuda:0", poison=False):
+        self.cfg = cfg
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("Expected a cuda device, but got: %s" % self.device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.dtype = torch_dtype("bf16" if cfg.dtype == LQ_BF16 else "f16")
+        self.sizes = logquant_sizes8(cfg)
+
+        def buf(nbytes):
+            return torch.full((int(nbytes),), 0xFF if poison else 0, dtype=torch.uint8, device=self.device)
+
+        for name in self.BUFFERS:
+            setattr(self, name, buf(getattr(self.sizes, name[2:])))
+        self.seq_state, self.workspace = buf(self.sizes.seq_state), buf(self.sizes.workspace)
+        self.n = (C.c_int32 * cfg.B)()
+        self.c = lq_cache8(*[getattr(self, name).data_ptr() for name in self.BUFFERS], C.cast(self.n, _I32P),
+                           self.seq_state.data_ptr())
+        self._call("logquant_workspace_init8", logquant_workspace_init8, self.cfg, self.workspace)
+
+    def _call(self, name, f, *args):
+        i = self.device.index
+        if torch.cuda.current_device() == i:
+            st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+        else:
+            with torch.cuda.device(i):
+                st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+        if st != LQ_OK:
+            raise LogQuantError(st, name)
+
+    def _check(self, name, t, *shape):
+        if t.shape != shape or t.dtype != self.dtype or t.device != self.device or not t.is_contiguous():
+            raise ValueError("%s: expected a contiguous %s tensor of shape %s on %s" % (name, self.dtype, shape, self.device))
+
+    def clone(self):
+        """A second cache with its own device buffers and the same contents and counts."""
+        other = DeviceCache8(self.cfg, self.device)
+        for name in self.BUFFERS:
+            getattr(other, name).copy_(getattr(self, name))
+        other.set_counts(self.counts())
+        return other
+
+    def counts(self):
+        return list(self.n)
+
+    def set_counts(self, counts):
+        """Set the host-side counts (the device buffers are left as they are)."""
+        self.n[:] = counts
+
+    def append(self, k_new, v_new, n_new=None):
+        """k_new, v_new: [B][Hkv][n][d]; n_new: tokens that each row takes of them, 0..n (None: all)."""
+        c = self.cfg
+        n = k_new.shape[2] if k_new.dim() == 4 else 1
+        self._check("k_new", k_new, c.B, c.Hkv, n, c.d)
+        self._check("v_new", v_new, c.B, c.Hkv, n, c.d)
+        if n_new is not None and len(n_new) != c.B:
+            raise ValueError("n_new: expected %d counts" % c.B)
+        self._call("logquant_append8", logquant_append8, c, self.c, k_new, v_new, n_new, n)
+
+    def read(self, t0, n, k_out=None, v_out=None):
+        """Tokens t0 .. t0+n-1 as ([B][Hkv][n][d], [B][Hkv][n][d]) tensors of the cache type: the given ones, whose rows
+        behind a sequence are left as they were, or new ones with zeros there."""
+        c = self.cfg
+        if n < 1:
+            raise LogQuantError(LQ_ERR_SHAPE, "logquant_read8")
+        k_out, v_out = (torch.zeros((c.B, c.Hkv, n, c.d), dtype=self.dtype, device=self.device) if t is None else t
+                        for t in (k_out, v_out))
+        self._check("k_out", k_out, c.B, c.Hkv, n, c.d)
+        self._check("v_out", v_out, c.B, c.Hkv, n, c.d)
+        self._call("logquant_read8", logquant_read8, c, self.c, t0, n, k_out, v_out)
+        return k_out, v_out
+
+    def decode_attn(self, q, out=None, softmax_scale=0.0):
+        """q: [B][Hq][d]; rows of the batch that hold no token give zeros."""
+        c = self.cfg
+        if out is None:
+            out = torch.empty_like(q)
+        self._check("q", q, c.B, c.Hq, c.d)
+        self._check("out", out, c.B, c.Hq, c.d)
+        self._call("logquant_decode_attn8", logquant_decode_attn8, c, self.c, q, softmax_scale, out, self.workspace)
+        return out
+
+    def decode_step(self, k_new, v_new, q, out=None, softmax_scale=0.0):
+        """Append one token per row ([B][Hkv][1][d]) and attend."""
+        c = self.cfg
+        if out is None:
+            out = torch.empty_like(q)
+        self._check("k_new", k_new, c.B, c.Hkv, 1, c.d)
+        self._check("v_new", v_new, c.B, c.Hkv, 1, c.d)
+        self._check("q", q, c.B, c.Hq, c.d)
+        self._check("out", out, c.B, c.Hq, c.d)
+        self._call("logquant_decode_step8", logquant_decode_step8, c, self.c, k_new, v_new, q, softmax_scale, out, self.workspace)
+        return out

@@ -1,0 +1,163 @@
+"""The 8-bit cache as append8 writes it and read8 reads it back, against the oracle, bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache8
+from tests import gpu_util8 as U
+
+pytestmark = pytest.mark.gpu
+CASES = [(d, G, dtype) for d in (64, 96, 128) for G in (32, 64, 128) for dtype in ("f16", "bf16")]
+
+
+def build(seed, B, Hq, Hkv, d, G, dtype, lengths, chunks=None, capacity=None):
+    """A device cache and its oracle with lengths[b] tokens, in one call or in calls of `chunks` tokens."""
+    top = max(lengths)
+    cache = U.make(B, Hq, Hkv, d, G, dtype, capacity or (top // G + 2) * G)
+    oracle = U.Oracle(cache, dtype)
+    K, V = U.rows(seed, B, Hkv, top, d, dtype), U.rows(seed + 1, B, Hkv, top, d, dtype, outliers=False)
+    oracle.append(K, V, lengths)
+    if chunks is None:
+        cache.append(K.to(U.DEVICE), V.to(U.DEVICE), lengths)
+    else:
+        at = 0
+        for n in chunks:
+            take = [max(0, min(n, x - at)) for x in lengths]
+            if max(take):
+                part = slice(at, at + n)
+                cache.append(K[:, :, part].contiguous().to(U.DEVICE), V[:, :, part].contiguous().to(U.DEVICE),
+                             [min(t, K[:, :, part].shape[2]) for t in take])
+            at += n
+    return cache, oracle
+
+
+@pytest.mark.parametrize("d,G,dtype", CASES)
+def test_a_prompt_of_rows_of_different_lengths(d, G, dtype):
+    cache, oracle = build(1, 5, 4, 2, d, G, dtype, [3 * G + 7, 2 * G, 0, 1, G - 1])
+    oracle.check(cache)
+
+
+@pytest.mark.parametrize("d,G,dtype", CASES[::5] + CASES[3::7])
+def test_the_state_does_not_depend_on_the_calls(d, G, dtype):
+    lengths = [4 * G + 5, 3 * G, 2 * G + 1, 17]
+    for chunks in ([1] * (4 * G + 5) if G == 32 else [G - 1, 2, 1, G, G + 1, 5 * G], [5, 2 * G - 5, 2 * G + 5], [G + 3] * 5, [3 * G + 1, G + 4]):
+        cache, oracle = build(11, 4, 2, 2, d, G, dtype, lengths, chunks)
+        oracle.check(cache)
+
+
+def test_more_rows_than_travel_in_a_launch():
+    rng = np.random.default_rng(3)
+    lengths = [int(x) for x in rng.integers(0, 100, 300)]
+    cache, oracle = build(21, 300, 2, 1, 64, 32, "f16", lengths)
+    oracle.check(cache)
+    assert all(torch.equal(a, b) for a, b in zip(cache.read(0, 100), cache.clone().read(0, 100)))
+
+
+def test_a_row_at_its_capacity():
+    cache, oracle = build(31, 2, 2, 2, 96, 64, "bf16", [256, 255], capacity=256)
+    oracle.check(cache)
+    k, v = cache.read(0, 256)
+    assert np.array_equal(U.f64(k[0, 1]), oracle.k[0][1].held()) and np.array_equal(U.f64(v[1, 0, :255]), oracle.v[1][0].held())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_values_at_the_ends_of_the_range(dtype):
+    """Blocks of zeros, of the type's smallest and largest numbers, of every 16-bit number, with ties of the rounding."""
+    G, d, dt = 32, 64, U.TYPES[dtype]
+    big = torch.finfo(dt).max
+    every = torch.arange(0, 2 ** 16, dtype=torch.int32).to(torch.int16).view(dt)
+    every = every[torch.isfinite(every)]
+    every = every[torch.randperm(len(every), generator=torch.Generator().manual_seed(1))]
+    parts = [torch.zeros(G * d), -torch.zeros(G * d), torch.full((G * d,), big), torch.full((G * d,), -big),
+             torch.linspace(-big, big, G * d), torch.full((G * d,), torch.finfo(dt).tiny), torch.linspace(-1, 1, G * d) * 448,
+             torch.arange(G * d).float() / 16 % 448, torch.arange(G * d).float() * 2.0 ** -11]
+    smallest = torch.arange(G * d, dtype=torch.int32).to(torch.int16).view(dt)             # subnormals
+    x = torch.cat([p.to(dt) for p in parts] + [smallest, every[:len(every) // (G * d) * (G * d)]])
+    x = torch.where(torch.isfinite(x), x, torch.full_like(x, big)).view(1, 1, -1, d)
+    # every 16-bit number in blocks of like magnitude too: sorted
+    srt = every.float().sort().values.to(dt)[:len(every) // (G * d) * (G * d)].view(1, 1, -1, d)
+    x = torch.cat([x, srt], 2)
+    cache = U.make(1, 1, 1, d, G, dtype, x.shape[2] + G)
+    oracle = U.Oracle(cache, dtype)
+    oracle.append(x, x.flip(2))
+    cache.append(x.to(U.DEVICE), x.flip(2).contiguous().to(U.DEVICE))
+    oracle.check(cache)
+    k, v = cache.read(0, x.shape[2])
+    assert np.array_equal(U.f64(k[0, 0]), oracle.k[0][0].held()) and np.array_equal(U.f64(v[0, 0]), oracle.v[0][0].held())
+
+
+@pytest.mark.parametrize("d,G,dtype", CASES[1::4] + [(96, 128, "bf16"), (64, 32, "f16")])
+def test_reading_ranges(d, G, dtype):
+    lengths = [3 * G + 9, 2 * G, 0, G - 1, 40]
+    cache, oracle = build(41, 5, 4, 2, d, G, dtype, lengths, capacity=5 * G)
+    full = [[(oracle.k[b][h].held(), oracle.v[b][h].held()) for h in range(2)] for b in range(5)]
+    ranges = [(0, 5 * G), (0, 1), (3 * G, 20), (G - 1, 2), (1, 3 * G - 3), (3 * G + 8, 1), (4 * G, G), (33, 31), (17, 2 * G), (5 * G - 1, 1)]
+    for t0, n in ranges:
+        mark = torch.full((5, 2, n, d), 7.0, dtype=cache.dtype, device=U.DEVICE)
+        ko, vo = mark.clone(), mark.clone()
+        got = cache.read(t0, n, ko, vo)
+        assert got[0] is ko and got[1] is vo
+        for b in range(5):
+            for h in range(2):
+                m = max(0, min(n, lengths[b] - t0))
+                assert np.array_equal(U.f64(ko[b, h, :m]), full[b][h][0][t0:t0 + m]), (t0, n, b, h)
+                assert np.array_equal(U.f64(vo[b, h, :m]), full[b][h][1][t0:t0 + m]), (t0, n, b, h)
+                assert (ko[b, h, m:] == 7).all() and (vo[b, h, m:] == 7).all()
+
+
+def test_reading_one_tensor_only():
+    from paper_2503_19950_amd import binding as B
+    cache, oracle = build(51, 2, 2, 1, 128, 64, "bf16", [100, 70])
+    want = cache.read(3, 90)
+    for which in range(2):
+        out = torch.zeros_like(want[0])
+        args = [None, None]
+        args[which] = out
+        assert B.logquant_read8(cache.cfg, cache.c, 3, 90, *args) == B.LQ_OK
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[which])
+
+
+def test_slices_beyond_4_gigabytes():
+    """Codes of the last rows lie past 2^32 bytes of their buffer."""
+    B, Hkv, d, G = 40, 8, 128, 128
+    cache = U.make(B, Hkv, Hkv, d, G, "bf16", 128 * 1024 + G)
+    assert cache.sizes.codes > 1 << 32
+    oracle = U.Oracle(cache, "bf16")
+    K, V = U.rows(61, B, Hkv, 3 * G + 5, d, "bf16"), U.rows(62, B, Hkv, 3 * G + 5, d, "bf16")
+    lengths = [0] * (B - 1) + [3 * G + 5]
+    lengths[0] = 2 * G
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), lengths)
+    oracle.append(K, V, lengths)
+    for b in (0, B - 1):
+        for h in (0, Hkv - 1):
+            U.check_state(cache, "k", b, h, oracle.k[b][h])
+            U.check_state(cache, "v", b, h, oracle.v[b][h])
+    q = U.rows(63, B, Hkv, 1, d, "bf16")[:, :, 0].contiguous()
+    U.check_output(cache.decode_attn(q.to(U.DEVICE)), q, oracle, "bf16", rows_of=[0, 1, B - 1])
+
+
+def test_tensors_of_another_kind_are_refused():
+    cache, _ = build(71, 2, 2, 1, 64, 32, "f16", [40, 3])
+    x = torch.zeros((2, 1, 4, 64), dtype=torch.float16, device=U.DEVICE)
+    q = torch.zeros((2, 2, 64), dtype=torch.float16, device=U.DEVICE)
+    one = x[:, :, :1].contiguous()
+    bad = [x.bfloat16(), x.cpu(), x[:1], x.transpose(2, 3), torch.zeros((2, 1, 4, 128), dtype=torch.float16, device=U.DEVICE)[..., ::2], x[0]]
+    for y in bad:
+        for args in ((x, y), (y, x)):
+            with pytest.raises(ValueError):
+                cache.append(*args)
+        with pytest.raises(ValueError):
+            cache.read(0, 4, y, x)
+        with pytest.raises(ValueError):
+            cache.decode_step(y, one, q)
+    for y in (q.bfloat16(), q.cpu(), q[:1], q[:, :1], q.transpose(0, 1)[:, :1]):
+        with pytest.raises(ValueError):
+            cache.decode_attn(y)
+        with pytest.raises(ValueError):
+            cache.decode_attn(q, y)
+        with pytest.raises(ValueError):
+            cache.decode_step(one, one, y)
+    with pytest.raises(ValueError):
+        cache.append(x, x, [1])
+    assert cache.counts() == [40, 3]
