@@ -386,7 +386,10 @@ lq_status logquant_workspace_init8(const lq_config8 *cfg, void *workspace, void 
  *   tokens are read; n_new : HOST array of B entries, 0 <= n_new[b] <= n_max (null: n_max
  *   for every row).
  * LQ_ERR_SHAPE for n_max < 1 or an n_new outside its range, LQ_ERR_CAPACITY if a row would
- * pass `capacity`.  On success n[b] += n_new[b]. */
+ * pass `capacity`.  On success n[b] += n_new[b].
+ * The caller may set n[b] back to drop tokens (a draft that was rejected) as far as the tail
+ * still holds the rows of the block that the new count ends in: that of the last n % G rows,
+ * or, when n % G == 0 after a call that filled up a block of the tail, that block's. */
 lq_status logquant_append8(const lq_config8 *cfg, lq_cache8 *cache, const void *k_new,
                            const void *v_new, const int32_t *n_new, int32_t n_max, void *stream);
 

@@ -1,6 +1,7 @@
 // C ABI of the 8-bit cache: argument checks on the host, then kernel launches.
 #include <math.h>
 
+#include <algorithm>
 #include <vector>
 
 #include "lq_cache8.h"
@@ -49,20 +50,27 @@ static RowArg8 row_arg(const lq_cache8* c, const std::vector<Row8>& rows) {
   return RowArg8{rows.data(), (Row8*)c->seq_state, (int)rows.size(), same};
 }
 
-static void plan8(const Shape8& s, std::vector<Row8>* rows, Plan8* p) {
+// Fills the rows' parts, first workgroups and order.  256 workgroups of 4 wavefronts read as fast as the memory delivers;
+// an item is split into parts of a 256th of all work (8 units at least, two to a wavefront), unless it is less than a 128th:
+// then its share of the time is smaller than what a join costs.
+static void plan8(const Shape8& s, bool same, std::vector<Row8>* rows, Plan8* p) {
   p->groups = head_groups8(s);
   p->hb = (s.gh + p->groups - 1) / p->groups;
-  int64_t work = 0;
-  for (Row8& r : *rows) {
-    r.x = (int)work;
-    work += units8(r.n, s.G);
-  }
   p->waves = 4;
-  p->total = (int)(work * s.Hkv * p->groups);
-  const int most = 512;
-  p->quota = (p->total + most - 1) / most;
-  if (p->quota < 4) p->quota = 4;
-  p->blocks = (p->total + p->quota - 1) / p->quota;
+  const int per_row = s.Hkv * p->groups;
+  int64_t work = 0;
+  for (const Row8& r : *rows) work += units8(r.n, s.G);
+  work *= per_row;
+  const int64_t most = std::max<int64_t>((work + 255) / 256, 8);
+  if (!same) std::sort(rows->begin(), rows->end(), [](const Row8& x, const Row8& y) { return x.n > y.n; });
+  int x = 0;
+  for (Row8& r : *rows) {
+    const int64_t u = units8(r.n, s.G);
+    r.parts = u * 128 <= work ? 1 : (int)std::max<int64_t>((u + most - 1) / most, 1);
+    r.x = x;
+    x += r.parts * per_row;
+  }
+  p->blocks = x;
 }
 
 static lq_status attend8(const Shape8& s, const lq_cache8& c, std::vector<Row8>* rows, const void* k_new, const void* v_new,
@@ -70,7 +78,7 @@ static lq_status attend8(const Shape8& s, const lq_cache8& c, std::vector<Row8>*
   bool same = true;
   for (const Row8& r : *rows) same = same && r.n == (*rows)[0].n;
   Plan8 plan;
-  plan8(s, rows, &plan);
+  plan8(s, same, rows, &plan);
   if (!(softmax_scale > 0.f)) softmax_scale = 1.0f / sqrtf((float)s.d);
   RowArg8 arg{rows->data(), (Row8*)c.seq_state, (int)rows->size(), same};
   return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, arg, stream) == hipSuccess ? LQ_OK : LQ_ERR_HIP;
@@ -89,7 +97,7 @@ lq_status logquant_sizes8(const lq_config8* cfg, lq_sizes8* out) {
   out->tail = bh * s.G * s.d * 2;
   out->seq_state = s.B * sizeof(Row8);
   const int groups = head_groups8(s);
-  out->workspace = counter_bytes8(s) + (size_t)2 * MAX_BLOCKS8 * partial_floats8((s.gh + groups - 1) / groups, s.d) * sizeof(float);
+  out->workspace = counter_bytes8(s) + (size_t)MAX_PARTS8 * partial_floats8((s.gh + groups - 1) / groups, s.d) * sizeof(float);
   return LQ_OK;
 }
 
@@ -116,7 +124,7 @@ lq_status logquant_append8(const lq_config8* cfg, lq_cache8* cache, const void* 
     const int take = n_new ? n_new[b] : n_max;
     if (take < 0 || take > n_max) return LQ_ERR_SHAPE;
     if (take > s.cap - cache->n[b]) return LQ_ERR_CAPACITY;
-    rows[b] = Row8{cache->n[b], take};
+    rows[b] = Row8{cache->n[b], take, 1, b};
     // a workgroup for each block that becomes full, and one for the rest, unless the first has rows in the tail (append8_kernel)
     const int held = cache->n[b] % s.G, full = (held + take) / s.G, rest = (held + take) % s.G;
     const int need = !take ? 0 : full + (rest && !(held && full) ? 1 : 0);
@@ -138,7 +146,7 @@ lq_status logquant_read8(const lq_config8* cfg, const lq_cache8* cache, int32_t 
   std::vector<Row8> rows(s.B);
   int longest = 0;
   for (int b = 0; b < s.B; ++b) {
-    rows[b] = Row8{cache->n[b], 0};
+    rows[b] = Row8{cache->n[b], 0, 1, b};
     if (cache->n[b] > longest) longest = cache->n[b];
   }
   if (longest <= t0) return LQ_OK;   // nothing of the range is there
@@ -154,7 +162,7 @@ lq_status logquant_decode_attn8(const lq_config8* cfg, const lq_cache8* cache, c
   if (st != LQ_OK) return st;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return LQ_ERR_SHAPE;
   std::vector<Row8> rows(s.B);
-  for (int b = 0; b < s.B; ++b) rows[b] = Row8{cache->n[b], 0};
+  for (int b = 0; b < s.B; ++b) rows[b] = Row8{cache->n[b], 0, 1, b};
   clear_stale_error();
   return attend8(s, *cache, &rows, nullptr, nullptr, q, softmax_scale, out, workspace, (hipStream_t)stream);
 }
@@ -170,13 +178,13 @@ lq_status logquant_decode_step8(const lq_config8* cfg, lq_cache8* cache, const v
   bool fills = false;
   for (int b = 0; b < s.B; ++b) {
     if (cache->n[b] == s.cap) return LQ_ERR_CAPACITY;
-    rows[b] = Row8{cache->n[b] + 1, 0};
+    rows[b] = Row8{cache->n[b] + 1, 0, 1, b};
     fills = fills || rows[b].n % s.G == 0;
   }
   clear_stale_error();
   if (fills) {   // a block has to be quantized before it is attended to
     std::vector<Row8> one(s.B);
-    for (int b = 0; b < s.B; ++b) one[b] = Row8{cache->n[b], 1};
+    for (int b = 0; b < s.B; ++b) one[b] = Row8{cache->n[b], 1, 1, b};
     if (launch_append8(s, *cache, k_new, v_new, 1, 1, row_arg(cache, one), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
     k_new = v_new = nullptr;
   }

@@ -39,7 +39,7 @@ template <typename P, int MODE>
 __device__ __forceinline__ Row8 row_of(const P& p, int b) {
   if constexpr (MODE == ROWS_SAME) return p.same;
   const Row8Ptr r = rows_ptr(p.rows, sizeof(P));
-  return Row8{r[b].n, r[b].x};
+  return Row8{r[b].n, r[b].x, 1, b};
 }
 
 // Magnitudes of a pair of values of T order like their 15 low bits as integers.
@@ -185,7 +185,10 @@ __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params
     }
   }
   if (i != tail_wg) return;
-  const int at = full ? 0 : held, left = all - full * G - at, from = full * G + at - held;   // slots at .. at + left - 1
+  // slots at .. at + left - 1 get the new rows from `from` on: the rows behind the last full block, or, where a block of the
+  // tail has just become full and nothing follows, its new rows, so that the count can be set back into it
+  const bool keep = held && all == G;
+  const int at = full && !keep ? 0 : held, left = (keep ? G : all - full * G) - at, from = keep ? 0 : full * G + at - held;
   for (int x = threadIdx.x; x < left * (D / 8); x += 64 * WAVES) {
     const int j = x / (D / 8), c = x % (D / 8) * 8;
     const int64_t src = (int64_t)(from + j) * D + c;

@@ -13,7 +13,7 @@
 // they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  The rounding to fp16 (2^-12 of each, unbiased) is
 // left out of the sum of the probabilities, which is kept in fp32.
 //
-// Bound by the bytes of the codes.  Work is dealt along one line (Plan8), inside a workgroup unit by unit to its wavefronts.
+// Bound by the bytes of the codes.  Workgroups take items or parts of them (Plan8), their wavefronts unit by unit.
 #include <type_traits>
 
 #include "lq_cache8.h"
@@ -48,8 +48,7 @@ struct Attn8Params {
   const Row8* rows;
   float scale;                               // softmax scale times log2(e)
   int B, Hkv, gh, groups, hb, log_g, cap;
-  int n, work;                               // ROWS_SAME: tokens and work of every row
-  int total, quota;
+  Row8 same;                                 // ROWS_SAME: every row's entry
 };
 
 __device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t rs, int off) {
@@ -107,297 +106,345 @@ __device__ __forceinline__ float head_sum(float v) {
 
 __device__ __forceinline__ float weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
 
-template <bool BF16, int D, int NW, int MODE>
-__global__ void __launch_bounds__(64 * NW) attn8_kernel(const Attn8Params P, const Rows8<MODE> S) {
+template <bool BF16, int D, int NW, int MODE, bool STEP>
+__global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, const Rows8<MODE> S) {
   (void)S;
   constexpr int ND = D / 32, NT = D / 16, PITCH = D + 4, UNIT = 32 * D;   // UNIT: bytes of a unit's codes
-  extern __shared__ __align__(16) float o_lds[];                     // [NW][hb][PITCH], m and l of a head behind its row
+  extern __shared__ __align__(16) float o_lds[];       // [NW][hb][PITCH], m and l of a head behind its row; or a join
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int a = lane / 16, head = lane % 16;
   const int per_row = P.Hkv * P.groups;                // items of a row
-  int x = blockIdx.x * P.quota;
-  const int end = x + P.quota < P.total ? x + P.quota : P.total;
-  bool first = true;
 
-  // the item at x, and the place in it
-  int b, j, n, work, pos;
-  const Row8Ptr rows = MODE == ROWS_SAME ? nullptr : rows_ptr(P.rows, sizeof(Attn8Params));
-  auto work_of = [&](int tokens) {
-    const int full = tokens >> P.log_g << P.log_g, u = full / 32 + 2 * ((tokens - full + 31) / 32);
-    return u > 0 ? u : 1;
-  };
+  // row, item j of it, part of the item
+  int b, n, parts, local;
   if constexpr (MODE == ROWS_SAME) {
-    n = P.n;
-    work = P.work;
-    const int item = x / work;
-    pos = x - item * work;
-    b = item / per_row;
-    j = item - b * per_row;
+    n = P.same.n;
+    parts = P.same.parts;
+    b = blockIdx.x / (per_row * parts);
+    local = blockIdx.x - b * per_row * parts;
   } else {
-    int before = 0;                                    // rows that begin at or before x
+    // The argument block lies in host memory: one load of all its rows, of which those are counted that begin here or before.
+    const Row8Ptr rows = rows_ptr(P.rows, sizeof(Attn8Params));
+    Row8 mine{};
     for (int i0 = 0; i0 < P.B; i0 += 64) {
       const int i = i0 + lane;
-      const bool le = i < P.B && rows[i].x * per_row <= x;
-      const int c = __popcll(__ballot(le));
-      before += c;
-      if (c < 64) break;
+      Row8 r{};
+      if (i < P.B) r = Row8{rows[i].n, rows[i].x, rows[i].parts, rows[i].b};
+      const int c = __popcll(__ballot(i < P.B && r.x <= (int)blockIdx.x));
+      if (!c) break;
+      mine = Row8{__builtin_amdgcn_readlane(r.n, c - 1), __builtin_amdgcn_readlane(r.x, c - 1),
+                  __builtin_amdgcn_readlane(r.parts, c - 1), __builtin_amdgcn_readlane(r.b, c - 1)};
     }
-    b = __builtin_amdgcn_readfirstlane(before - 1);
-    n = rows[b].n;
-    work = work_of(n);
-    const int local = x - rows[b].x * per_row;
-    j = local / work;
-    pos = local - j * work;
+    n = mine.n;
+    parts = mine.parts;
+    b = mine.b;
+    local = blockIdx.x - mine.x;
+  }
+  const int j = local / parts, part = local - j * parts;
+  const int codes = n >> P.log_g << (P.log_g - 5), rest = n - 32 * codes;   // units of codes, rows of the tail
+  const int work = codes + 2 * ((rest + 31) / 32), size = (work + parts - 1) / parts;
+  const int pos = part * size, to = pos + size < work ? pos + size : work;
+  const int h = j / P.groups, g = j - h * P.groups;
+  const int64_t bh = (int64_t)b * P.Hkv + h;
+  const int heads = P.hb < P.gh - g * P.hb ? P.hb : P.gh - g * P.hb;
+  const int64_t head0 = bh * P.gh + g * P.hb;
+
+  u32x4 q[ND];
+  {
+    const __amdgpu_buffer_rsrc_t rs = buffer(P.q + head0 * D, heads * D * 2);   // absent heads: zeros
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) q[nd] = load16(rs, head * D * 2 + a * 16 + nd * 64);
   }
 
-  while (x < end) {
-    const int to = pos + (end - x) < work ? pos + (end - x) : work;       // [pos, to) of this item is ours
-    const int h = j / P.groups, g = j - h * P.groups;
-    const int64_t bh = (int64_t)b * P.Hkv + h;
-    const int heads = P.hb < P.gh - g * P.hb ? P.hb : P.gh - g * P.hb;
-    const int64_t head0 = bh * P.gh + g * P.hb;
-    const int full = n >> P.log_g << P.log_g, codes = full / 32, rest = n - full;
+  // Units of the tail that are ours go to the last wavefronts, one each, which sit out the first two rounds of codes.
+  int tails = 0;
+  for (int i = 0; 32 * i < rest; ++i) tails += codes + 2 * i >= pos && codes + 2 * i < to;
+  const int skip = pos > codes ? (pos - codes + 1) / 2 : 0;               // units of the tail before ours
+  const int tail_unit = skip + NW - 1 - wave;
+  const bool has_tail = NW - 1 - wave < tails;
+  const int workers = tails < NW ? NW - tails : NW;                       // wavefronts in the first two rounds
+  const int stop = to < codes ? to : codes;
+  int i = pos + (wave < workers ? wave : wave + 2 * workers), round = wave < workers ? 0 : 2;
 
-    u32x4 q[ND];
-    {
-      const __amdgpu_buffer_rsrc_t rs = buffer(P.q + head0 * D, heads * D * 2);   // absent heads: zeros
+  const __amdgpu_buffer_rsrc_t rk = buffer(P.k_codes + bh * P.cap * D, stop * UNIT);   // behind the last unit: zeros, no reads
+  const __amdgpu_buffer_rsrc_t rv = buffer(P.v_codes + bh * P.cap * D, stop * UNIT);
+  typedef const float __attribute__((address_space(4))) * ScalePtr;      // read by scalar loads
+  const ScalePtr ks = (ScalePtr)(uintptr_t)(P.k_scale + bh * (P.cap >> P.log_g));
+  const ScalePtr vs = (ScalePtr)(uintptr_t)(P.v_scale + bh * (P.cap >> P.log_g));
+  u32x4 k[ND], v[ND];
+  float ck, cv;
+  auto load_k = [&]() {
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) q[nd] = load16(rs, head * D * 2 + a * 16 + nd * 64);
+    for (int nd = 0; nd < ND; ++nd) k[nd] = load16(rk, i * UNIT + lane * 16 + nd * 1024);
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) v[nd] = load16(rv, i * UNIT + lane * 16 + nd * 1024);
+  };
+  auto load_scales = [&]() {
+    const int block = i < stop ? i >> (P.log_g - 5) : 0;
+    ck = ks[block];
+    cv = vs[block];
+  };
+
+  f32x4 acc[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  // a lane's largest logit of a unit: when it is over the reference by more than SLACK anywhere, a new reference
+  auto look_up = [&](float top) {
+    if (__any(top > m + SLACK)) {
+      const float now = fmaxf(m, head_max(top)), f = weight(m, now);
+      m = now;
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t] *= f;
     }
-    f32x4 acc[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
+  };
 
-    // a lane's largest logit of a unit: when it is over the reference by more than SLACK anywhere, a new reference
-    auto look_up = [&](float top) {
-      if (__any(top > m + SLACK)) {
-        const float now = fmaxf(m, head_max(top)), f = weight(m, now);
-        m = now;
-        l *= f;
+  // ---- rows of the tail
+  if (has_tail) {
+    const int left = rest - 32 * tail_unit, live = left < 32 ? left : 32;
+    uint16_t* k_tail = P.k_tail + (bh << P.log_g) * D;
+    uint16_t* v_tail = P.v_tail + (bh << P.log_g) * D;
+    u32x4 kt[2 * ND], vt[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t] *= f;
-      }
-    };
-
-    // ---- codes
-    const int stop = to < codes ? to : codes;
-    const __amdgpu_buffer_rsrc_t rk = buffer(P.k_codes + bh * P.cap * D, stop * UNIT);   // behind the last unit: no reads
-    const __amdgpu_buffer_rsrc_t rv = buffer(P.v_codes + bh * P.cap * D, stop * UNIT);
-    const float* ks = P.k_scale + bh * (P.cap >> P.log_g);
-    const float* vs = P.v_scale + bh * (P.cap >> P.log_g);
-    struct Unit { u32x4 k[ND], v[ND]; float ks, vs; };
-    auto load = [&](Unit& u, int i) {
+    for (int t = 0; t < 2 * ND; ++t) kt[t] = *reinterpret_cast<const u32x4*>(k_tail + 32 * tail_unit * D + (t * 64 + lane) * 8);
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) u.k[nd] = load16(rk, i * UNIT + lane * 16 + nd * 1024);
+    for (int t = 0; t < NT; ++t) vt[t] = *reinterpret_cast<const u32x4*>(v_tail + 32 * tail_unit * D + (t * 64 + lane) * 8);
+    if constexpr (STEP) {                            // the new row takes its place, here and (every head group) in the cache
+      if (left <= 32) {
+        const int t = left - 1, r = 32 * tail_unit + t, e = 4 * (t / 16) + t % 4;
+        u32x4 k_new[ND];
+        uint16_t v_new[NT];
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) u.v[nd] = load16(rv, i * UNIT + lane * 16 + nd * 1024);
-      const int block = (i < stop ? i : stop - 1) >> (P.log_g - 5);
-      u.ks = ks[block];
-      u.vs = vs[block];
-    };
-    auto attend = [&](const Unit& u) {
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+        for (int nd = 0; nd < ND; ++nd) k_new[nd] = *reinterpret_cast<const u32x4*>(P.k_new + bh * D + 32 * nd + 8 * a);
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) {
-        s0 = mfma<BF16>(codes_as<BF16>(u.k[nd][0], u.k[nd][1]), q[nd], s0);
-        s1 = mfma<BF16>(codes_as<BF16>(u.k[nd][2], u.k[nd][3]), q[nd], s1);
-      }
-      const float c = u.ks * P.scale;
-      look_up(fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3]))) * c);
-      float p[8];
+        for (int n = 0; n < NT; ++n) v_new[n] = P.v_new[bh * D + 16 * n + head];
+        if (head == t % 16) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(e < 4 ? s0[e] : s1[e - 4], c, BIAS - m));
-        l += p[e];
-      }
-      const u32x4 pb = {pair_as<false>(p[0], p[1]), pair_as<false>(p[2], p[3]), pair_as<false>(p[4], p[5]), pair_as<false>(p[6], p[7])};
+          for (int nd = 0; nd < ND; ++nd) {
+            if (t < 16) kt[nd] = k_new[nd]; else kt[ND + nd] = k_new[nd];
+            *reinterpret_cast<u32x4*>(k_tail + k_fp_index(r, 32 * nd + 8 * a, ND)) = k_new[nd];
+          }
+        }
+        if (a == t % 16 / 4) {
+          const uint32_t mask = e & 1 ? 0xFFFF0000u : 0xFFFFu;
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) {
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        const f32x4 o0 = mfma<false>(codes_as<false>(u.v[nd][0], u.v[nd][1]), pb, zero);
-        const f32x4 o1 = mfma<false>(codes_as<false>(u.v[nd][2], u.v[nd][3]), pb, zero);
+          for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc[2 * nd][e] = fmaf(o0[e], u.vs, acc[2 * nd][e]);
-          acc[2 * nd + 1][e] = fmaf(o1[e], u.vs, acc[2 * nd + 1][e]);
+            for (int w = 0; w < 4; ++w)
+              if (w == e / 2) vt[n][w] = (vt[n][w] & ~mask) | ((v_new[n] * 0x10001u) & mask);
+            v_tail[v_fp_index(r, 16 * n + head, NT)] = v_new[n];
+          }
         }
       }
-    };
-    if (pos + wave < stop) {
-      Unit u0, u1;
-      int i = pos + wave;
-      load(u0, i);
-      while (true) {
-        load(u1, i + NW);
-        attend(u0);
-        i += NW;
-        if (i >= stop) break;
-        load(u0, i + NW);
-        attend(u1);
-        i += NW;
-        if (i >= stop) break;
+    }
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) {
+      s0 = mfma<BF16>(kt[nd], q[nd], s0);
+      s1 = mfma<BF16>(kt[ND + nd], q[nd], s1);
+    }
+    float z[8], top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      z[e] = 16 * (e / 4) + 4 * a + e % 4 < live ? (e < 4 ? s0[e] : s1[e - 4]) * P.scale : -INFINITY;
+      top = fmaxf(top, z[e]);
+    }
+    look_up(top);
+    float p[8], r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m));
+      l += p[e];
+    }
+    // a bf16 operand keeps 8 bits of a probability: the rest goes in as a second one
+    const u32x4 pb = {pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(pb[e / 2] >> (16 * (e & 1))));
+    const u32x4 pr = {pair_as<BF16>(r[0], r[1]), pair_as<BF16>(r[2], r[3]), pair_as<BF16>(r[4], r[5]), pair_as<BF16>(r[6], r[7])};
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {                  // rows that are not there have weight 0, but may hold anything
+        const int t0 = 16 * (w / 2) + 4 * a + 2 * (w % 2);
+        vt[t][w] &= (t0 < live ? 0xFFFFu : 0u) | (t0 + 1 < live ? 0xFFFF0000u : 0u);
+      }
+      acc[t] = mfma<BF16>(vt[t], pb, acc[t]);
+      if constexpr (BF16) acc[t] = mfma<BF16>(vt[t], pr, acc[t]);
+    }
+  }
+
+  // ---- codes; the keys of the next unit are under way while the values of this one are used
+  if (i < stop) {
+    load_k();
+    load_scales();
+    load_v();
+  }
+  while (i < stop) {
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) {
+      s0 = mfma<BF16>(codes_as<BF16>(k[nd][0], k[nd][1]), q[nd], s0);
+      s1 = mfma<BF16>(codes_as<BF16>(k[nd][2], k[nd][3]), q[nd], s1);
+    }
+    const float c = ck * P.scale, f = cv;
+    i += round < 2 ? workers : NW;
+    ++round;
+    load_k();
+    load_scales();
+    look_up(fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3]))) * c);
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(fmaf(e < 4 ? s0[e] : s1[e - 4], c, BIAS - m));
+      l += p[e];
+    }
+    const u32x4 pb = {pair_as<false>(p[0], p[1]), pair_as<false>(p[2], p[3]), pair_as<false>(p[4], p[5]), pair_as<false>(p[6], p[7])};
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) {
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      const f32x4 o0 = mfma<false>(codes_as<false>(v[nd][0], v[nd][1]), pb, zero);
+      const f32x4 o1 = mfma<false>(codes_as<false>(v[nd][2], v[nd][3]), pb, zero);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[2 * nd][e] = fmaf(o0[e], f, acc[2 * nd][e]);
+        acc[2 * nd + 1][e] = fmaf(o1[e], f, acc[2 * nd + 1][e]);
       }
     }
-
-    // ---- rows of the tail, from the last wavefront down
-    for (int i = NW - 1 - wave; 32 * i < rest; i += NW) {
-      const int at = codes + 2 * i;
-      if (at < pos || at >= to) continue;
-      uint16_t* k_tail = P.k_tail + (bh << P.log_g) * D;
-      uint16_t* v_tail = P.v_tail + (bh << P.log_g) * D;
-      if (P.k_new && 32 * i + 32 >= rest) {            // the new row first; every head group stores the same
-        const int t = rest - 1;
-        if (lane < D / 8)
-          *reinterpret_cast<u32x4*>(k_tail + k_fp_index(t, 8 * lane, ND)) = *reinterpret_cast<const u32x4*>(P.k_new + bh * D + 8 * lane);
-        for (int c = lane; c < D; c += 64) v_tail[v_fp_index(t, c, NT)] = P.v_new[bh * D + c];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        __builtin_amdgcn_s_waitcnt(0);
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-      }
-      const int live = rest - 32 * i < 32 ? rest - 32 * i : 32;
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+    load_v();
+  }
+  // ---- the workgroup's wavefronts together
+  l = head_sum(l);
+  if (head < heads) {
+    float* mine = o_lds + (wave * P.hb + head) * PITCH;
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) {
-        s0 = mfma<BF16>(*reinterpret_cast<const u32x4*>(k_tail + (((2 * i) * ND + nd) * 64 + lane) * 8), q[nd], s0);
-        s1 = mfma<BF16>(*reinterpret_cast<const u32x4*>(k_tail + (((2 * i + 1) * ND + nd) * 64 + lane) * 8), q[nd], s1);
-      }
-      float z[8], top = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        z[e] = 16 * (e / 4) + 4 * a + e % 4 < live ? (e < 4 ? s0[e] : s1[e - 4]) * P.scale : -INFINITY;
-        top = fmaxf(top, z[e]);
-      }
-      look_up(top);
-      float p[8], r[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m));
-        l += p[e];
-      }
-      // a bf16 operand keeps 8 bits of a probability: the rest goes in as a second one
-      const u32x4 pb = {pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(pb[e / 2] >> (16 * (e & 1))));
-      const u32x4 pr = {pair_as<BF16>(r[0], r[1]), pair_as<BF16>(r[2], r[3]), pair_as<BF16>(r[4], r[5]), pair_as<BF16>(r[6], r[7])};
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        u32x4 v = *reinterpret_cast<const u32x4*>(v_tail + ((i * NT + t) * 64 + lane) * 8);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {                  // rows that are not there have weight 0, but may hold anything
-          const int t0 = 16 * (w / 2) + 4 * a + 2 * (w % 2);
-          v[w] &= (t0 < live ? 0xFFFFu : 0u) | (t0 + 1 < live ? 0xFFFF0000u : 0u);
-        }
-        acc[t] = mfma<BF16>(v, pb, acc[t]);
-        if constexpr (BF16) acc[t] = mfma<BF16>(v, pr, acc[t]);
-      }
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(mine + 16 * t + 4 * a) = acc[t];
+    if (a == 0) {
+      mine[D] = m;
+      mine[D + 1] = l;
     }
-
-    // ---- the workgroup's wavefronts together
-    l = head_sum(l);
-    if (head < heads) {
-      float* mine = o_lds + (wave * P.hb + head) * PITCH;
+  }
+  __syncthreads();
+  const int slot = P.hb * PITCH;                     // floats of a partial result
+  const __amdgpu_buffer_rsrc_t rp = buffer(P.partials + (int64_t)blockIdx.x * slot, slot * 4);
+  auto write_out = [&](int hd, int c, f32x4 o, float sum) {
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    *reinterpret_cast<u32x2*>(P.out + (head0 + hd) * D + c) =
+        u32x2{pair_as<BF16>(o[0] * inv, o[1] * inv), pair_as<BF16>(o[2] * inv, o[3] * inv)};
+  };
+  for (int i = threadIdx.x; i < heads * (D / 4); i += 64 * NW) {
+    const int hd = i / (D / 4), c = 4 * (i % (D / 4));
+    float top = -INFINITY, sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(mine + 16 * t + 4 * a) = acc[t];
-      if (a == 0) {
-        mine[D] = m;
-        mine[D + 1] = l;
-      }
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, o_lds[(w * P.hb + hd) * PITCH + D]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float* row = o_lds + (w * P.hb + hd) * PITCH;
+      const float f = weight(row[D], top);
+      sum = fmaf(row[D + 1], f, sum);
+      o += *reinterpret_cast<const f32x4*>(row + c) * f;
+    }
+    if (parts == 1) {
+      write_out(hd, c, o, sum);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rp, (hd * PITCH + c) * 4, 0, DEVICE_COHERENT);
+      if (c == 0)
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(top), __float_as_uint(sum)}, rp, (hd * PITCH + D) * 4, 0, DEVICE_COHERENT);
+    }
+  }
+
+  // ---- the workgroups of an item together: the last one to come joins them, nobody waits
+  if (parts > 1) {
+    __shared__ int last;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);                   // the partial results are where the other dies see them
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int* ctr = P.counters + (int64_t)(b * per_row + j) * CTR8;
+      last = __hip_atomic_fetch_add(ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+      if (last) __hip_atomic_store(ctr, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
     }
     __syncthreads();
-    const bool whole = pos == 0 && to == work;
-    const int slot = P.hb * PITCH;                     // floats of a partial result
-    const __amdgpu_buffer_rsrc_t rp = buffer(P.partials + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * slot, slot * 4);
-    auto write_out = [&](int hd, int c, f32x4 o, float sum) {
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
-      *reinterpret_cast<u32x2*>(P.out + (head0 + hd) * D + c) =
-          u32x2{pair_as<BF16>(o[0] * inv, o[1] * inv), pair_as<BF16>(o[2] * inv, o[3] * inv)};
-    };
-    for (int i = threadIdx.x; i < heads * (D / 4); i += 64 * NW) {
-      const int hd = i / (D / 4), c = 4 * (i % (D / 4));
-      float top = -INFINITY, sum = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (last) {
+      // Every thread takes four channels of a head and, where there are more threads than those, a share of the parts;
+      // eight parts' loads are under way at a time.
+      constexpr int T = 64 * NW, BATCH = 8;
+      const __amdgpu_buffer_rsrc_t rs = buffer(P.partials + (int64_t)(blockIdx.x - part) * slot, parts * slot * 4);
+      const int cols = heads * (D / 4), shares = cols < T ? T / cols : 1;
+      for (int i = threadIdx.x; i < cols * shares; i += T) {
+        const int share = i / cols, col = i - share * cols, hd = col / (D / 4), c = 4 * (col % (D / 4));
+        float top = -INFINITY, sum = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int k0 = share; k0 < parts; k0 += BATCH * shares) {
+          u32x4 y[BATCH];
+          u32x2 ml[BATCH];
 #pragma unroll
-      for (int w = 0; w < NW; ++w) top = fmaxf(top, o_lds[(w * P.hb + hd) * PITCH + D]);
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float* row = o_lds + (w * P.hb + hd) * PITCH;
-        const float f = weight(row[D], top);
-        sum = fmaf(row[D + 1], f, sum);
-        o += *reinterpret_cast<const f32x4*>(row + c) * f;
-      }
-      if (whole) {
-        write_out(hd, c, o, sum);
-      } else {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rp, (hd * PITCH + c) * 4, 0, DEVICE_COHERENT);
-        if (c == 0)
-          __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(top), __float_as_uint(sum)}, rp, (hd * PITCH + D) * 4, 0, DEVICE_COHERENT);
-      }
-    }
-
-    // ---- the workgroups of an item together: the last one to come joins them, nobody waits
-    if (!whole) {
-      __shared__ int last;
-      const int start = x - pos, w0 = start / P.quota, parts = (start + work - 1) / P.quota - w0 + 1;
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-      __builtin_amdgcn_s_waitcnt(0);                   // the partial results are where the other dies see them
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        int* ctr = P.counters + (int64_t)(b * per_row + j) * CTR8;
-        last = __hip_atomic_fetch_add(ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
-        if (last) __hip_atomic_store(ctr, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
-      }
-      __syncthreads();
-      if (last) {
-        // w0 had the item as its last, the others as their first
-        const float* base = P.partials + ((int64_t)w0 * 2) * slot;
-        const __amdgpu_buffer_rsrc_t rs = buffer(base, parts * 2 * slot * 4);
-        const int skip = start == w0 * P.quota ? 0 : slot;
-        for (int i = threadIdx.x; i < heads * (D / 4); i += 64 * NW) {
-          const int hd = i / (D / 4), c = 4 * (i % (D / 4));
-          float top = -INFINITY, sum = 0.f;
-          f32x4 o = {0.f, 0.f, 0.f, 0.f};
-          for (int k = 0; k < parts; ++k) {
-            const int off = (2 * k * slot + (k ? 0 : skip) + hd * PITCH) * 4;
-            const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rs, off + c * 4, 0, DEVICE_COHERENT);
-            const u32x2 ml = __builtin_amdgcn_raw_buffer_load_b64(rs, off + D * 4, 0, DEVICE_COHERENT);
-            const float now = fmaxf(top, __uint_as_float(ml[0]));
-            const float f0 = weight(top, now), f1 = weight(__uint_as_float(ml[0]), now);
-            sum = sum * f0 + __uint_as_float(ml[1]) * f1;
-            o = o * f0 + __builtin_bit_cast(f32x4, y) * f1;
-            top = now;
+          for (int e = 0; e < BATCH; ++e) {          // behind the last part: zeros, not read
+            const int k = k0 + e * shares, off = (k * slot + hd * PITCH) * 4;
+            ml[e] = __builtin_amdgcn_raw_buffer_load_b64(rs, off + D * 4, 0, DEVICE_COHERENT);
+            y[e] = __builtin_amdgcn_raw_buffer_load_b128(rs, off + c * 4, 0, DEVICE_COHERENT);
           }
+          float now = top;
+#pragma unroll
+          for (int e = 0; e < BATCH; ++e)
+            if (k0 + e * shares < parts) now = fmaxf(now, __uint_as_float(ml[e][0]));
+          const float f = weight(top, now);
+          sum *= f;
+          o *= f;
+          top = now;
+#pragma unroll
+          for (int e = 0; e < BATCH; ++e) {
+            const float g = k0 + e * shares < parts ? weight(__uint_as_float(ml[e][0]), now) : 0.f;
+            sum = fmaf(__uint_as_float(ml[e][1]), g, sum);
+            o += __builtin_bit_cast(f32x4, y[e]) * g;
+          }
+        }
+        if (shares > 1) {                            // (then this is the thread's only column)
+          *reinterpret_cast<f32x4*>(o_lds + 4 * i) = o;
+          o_lds[4 * T + i] = top;
+          o_lds[5 * T + i] = sum;
+        } else {
           write_out(hd, c, o, sum);
         }
       }
-    }
-    __syncthreads();                                   // o_lds and `last` are free again
-
-    x += to - pos;
-    pos = 0;
-    first = false;
-    if (++j == per_row) {
-      j = 0;
-      ++b;
-      if (MODE == ROWS_LISTED && x < end) {
-        n = rows[b].n;
-        work = work_of(n);
+      if (shares > 1) {
+        __syncthreads();
+        const int col = threadIdx.x;
+        if (col < cols) {
+          float top = -INFINITY, sum = 0.f;
+          f32x4 o = {0.f, 0.f, 0.f, 0.f};
+          for (int k = 0; k < shares; ++k) top = fmaxf(top, o_lds[4 * T + k * cols + col]);
+          for (int k = 0; k < shares; ++k) {
+            const float f = weight(o_lds[4 * T + k * cols + col], top);
+            sum = fmaf(o_lds[5 * T + k * cols + col], f, sum);
+            o += *reinterpret_cast<const f32x4*>(o_lds + 4 * (k * cols + col)) * f;
+          }
+          write_out(col / (D / 4), 4 * (col % (D / 4)), o, sum);
+        }
       }
     }
   }
 }
 
-template <int MODE>
+template <int MODE, bool STEP>
 hipError_t attn8(const Shape8& s, const Attn8Params& p, const Rows8<MODE>& rows, const Plan8& plan, hipStream_t st) {
-  constexpr int NW = 4;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(64 * NW), NW * partial_floats8(plan.hb, s.d) * sizeof(float), st, p, rows);
+    const int floats = plan.waves * partial_floats8(plan.hb, s.d), join = plan.waves * 64 * 6;
+    hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(64 * plan.waves), (floats > join ? floats : join) * sizeof(float), st, p, rows);
+  };
+  auto with_waves = [&](auto bf16, auto waves) {
+    constexpr bool T = decltype(bf16)::value;
+    constexpr int NW = decltype(waves)::value;
+    if (s.d == 64) return go(attn8_kernel<T, 64, NW, MODE, STEP>);
+    if (s.d == 96) return go(attn8_kernel<T, 96, NW, MODE, STEP>);
+    go(attn8_kernel<T, 128, NW, MODE, STEP>);
   };
   auto with_type = [&](auto bf16) {
-    constexpr bool T = decltype(bf16)::value;
-    if (s.d == 64) return go(attn8_kernel<T, 64, NW, MODE>);
-    if (s.d == 96) return go(attn8_kernel<T, 96, NW, MODE>);
-    go(attn8_kernel<T, 128, NW, MODE>);
+    with_waves(bf16, std::integral_constant<int, 4>{});
   };
   if (s.bf16) with_type(std::true_type{}); else with_type(std::false_type{});
   return launch_status("attn8");
@@ -409,12 +456,16 @@ hipError_t launch_attn8(const Shape8& s, const lq_cache8& c, const void* q, floa
                         const void* k_new, const void* v_new, const RowArg8& rows, hipStream_t st) {
   Attn8Params p{(const uint16_t*)q, (uint16_t*)out, c.k_codes, c.v_codes, c.k_scale, c.v_scale, (uint16_t*)c.k_tail, (uint16_t*)c.v_tail,
                 (const uint16_t*)k_new, (const uint16_t*)v_new, (int*)ws, (float*)((char*)ws + counter_bytes8(s)), nullptr,
-                scale * 1.44269504088896340736f, s.B, s.Hkv, s.gh, plan.groups, plan.hb, log2_of(s.G), s.cap, rows.host[0].n,
-                units8(rows.host[0].n, s.G), plan.total, plan.quota};
-  if (rows.same) return attn8<ROWS_SAME>(s, p, Rows8<ROWS_SAME>{}, plan, st);
+                scale * 1.44269504088896340736f, s.B, s.Hkv, s.gh, plan.groups, plan.hb, log2_of(s.G), s.cap,
+                rows.host[0]};
+  if (rows.same) {
+    const Rows8<ROWS_SAME> none;
+    return k_new ? attn8<ROWS_SAME, true>(s, p, none, plan, st) : attn8<ROWS_SAME, false>(s, p, none, plan, st);
+  }
   Rows8<ROWS_LISTED> listed{};
   const hipError_t e = hand_over(rows, &listed, &p.rows, st);
-  return e != hipSuccess ? e : attn8<ROWS_LISTED>(s, p, listed, plan, st);
+  if (e != hipSuccess) return e;
+  return k_new ? attn8<ROWS_LISTED, true>(s, p, listed, plan, st) : attn8<ROWS_LISTED, false>(s, p, listed, plan, st);
 }
 
 }  // namespace lq

@@ -17,9 +17,11 @@ inline int log2_of(int G) { return G == 32 ? 5 : G == 64 ? 6 : 7; }
 // What a launch has to know of a batch row.
 struct Row8 {
   int n;               // tokens that the row holds (append: before the call; a fused step: after it)
-  int x;               // append: tokens that it takes; attention: work of a head of all rows before it (Plan8)
+  int x;               // append: tokens that it takes; attention: its first workgroup
+  int parts;           // attention: workgroups that share an item of it (Plan8)
+  int b;               // attention: which row
 };
-// Up to so many rows (1 KB) travel in the launch's own arguments; more are uploaded into the cache's device scratch
+// Up to so many rows (2 KB) travel in the launch's own arguments; more are uploaded into the cache's device scratch
 // first, on the same stream.  Rows that are all alike travel as one entry.
 constexpr int ROWS_IN_ARGS = 128;
 typedef const Row8 __attribute__((address_space(4))) * Row8Ptr;
@@ -54,16 +56,15 @@ __device__ __forceinline__ Row8Ptr rows_ptr(const Row8* dev, size_t offset) {
 }
 
 // How attention is dealt to workgroups.  A (row, kv head, head group) is an item; its work is counted in units of 32
-// tokens, codes as 1 and rows of the tail, twice as wide, as 2, at least 1 (an empty row's output is written as well).
-// The work of all items lies on one line, row by row, and workgroup w takes [w * quota, (w + 1) * quota) of it, so rows of
-// any lengths load the chip evenly; an item that several workgroups share is joined by the last of them.
+// tokens, codes as 1 and rows of the tail, twice as wide, as 2.  A workgroup takes an item, or one of `parts` equal parts
+// of it, which the last of them to finish joins.  Rows with the most work come first.
 struct Plan8 {
   int groups, hb;      // head groups of a kv head; heads in each (at most 16, the columns of an operand; the last has the rest)
-  int total, quota, blocks, waves;
+  int blocks, waves;
 };
 inline int units8(int n, int G) {
-  const int full = n / G * G, u = full / 32 + 2 * ((n - full + 31) / 32);
-  return u > 0 ? u : 1;
+  const int full = n / G * G;
+  return full / 32 + 2 * ((n - full + 31) / 32);
 }
 
 hipError_t launch_append8(const Shape8& s, const lq_cache8& c, const void* k_new, const void* v_new, int n_max, int blocks,
@@ -73,9 +74,10 @@ hipError_t launch_read8(const Shape8& s, const lq_cache8& c, int t0, int n, void
 hipError_t launch_attn8(const Shape8& s, const lq_cache8& c, const void* q, float scale, void* out, void* ws, const Plan8& plan,
                         const void* k_new, const void* v_new, const RowArg8& rows, hipStream_t st);
 
-// A workspace: the counters of the items, one to a cache line, then room for two partial results of every workgroup.
+// A workspace: the counters of the items, one to a cache line, then room for the partial results of the workgroups that
+// share an item (they come first in the grid).
 constexpr int CTR8 = 32;           // ints from one counter to the next
-constexpr int MAX_BLOCKS8 = 1024;
+constexpr int MAX_PARTS8 = 1024;
 inline int head_groups8(const Shape8& s) { return (s.gh + 15) / 16; }
 inline size_t counter_bytes8(const Shape8& s) { return (size_t)s.B * s.Hkv * head_groups8(s) * CTR8 * sizeof(int); }
 inline int partial_floats8(int hb, int d) { return hb * (d + 4); }   // o, then m and l, padded to 16 bytes
