@@ -4,7 +4,7 @@
 // works on pieces of 32 tokens x 32 channels, which are 1 KB of codes in one stretch, 16 bytes a lane.  Keys: a lane holds
 // eight channels of tokens t and t + 16, as they lie in a row of the prompt.  Values: a lane needs eight tokens of two
 // channels c and c + 16; it loads two neighbouring channels of eight tokens (4 bytes each, 64 in a row per 16 lanes) and
-// trades half of the packed codes with the lane eight places away, so nothing goes through LDS.
+// trades half of the packed codes with the lane eight places away.
 #include "lq_cache8.h"
 #include "lq_device.h"
 #include "lq_internal.h"
@@ -81,6 +81,13 @@ __device__ __forceinline__ uint32_t values2(uint32_t w, bool hi, float scale) {
 
 __device__ __forceinline__ uint32_t other_half_row(uint32_t v) {   // of the lane eight places away in a row of 16
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false);
+}
+
+// Order of LDS accesses within a wavefront (its LDS instructions execute in order: only the compiler has to be told).
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // token within its unit of 32 at position e of the eight that lane row a holds: 16 b + 4 a + e % 4, b = e / 4
@@ -217,46 +224,64 @@ __global__ void __launch_bounds__(64 * WAVES) read8_kernel(const Read8Params P, 
   if (32 * unit < full) {
     const int64_t slice = ((int64_t)bh * P.cap + 32 * (int64_t)unit) * D;
     const int64_t block = (int64_t)bh * (P.cap >> P.log_g) + (32 * unit >> P.log_g);
-    if (P.k_out) {
-      const float s = P.k_scale[block];
-      uint4 w[ND];
+    const bool upper = lane & 8;
+    const int cc = 2 * (lane & 7) + (upper ? 1 : 0);
+    uint4 k[ND], v[ND];
+    if (P.k_out)
 #pragma unroll
-      for (int nd = 0; nd < ND; ++nd) w[nd] = *reinterpret_cast<const uint4*>(P.k_codes + slice + nd * 1024 + lane * 16);
-#pragma unroll
-      for (int nd = 0; nd < ND; ++nd) {
-        const int t = 32 * unit + lane % 16, c = 32 * nd + 8 * (lane / 16);
-        auto row8 = [&](uint32_t a, uint32_t b) {
-          return make_uint4(values2<BF16>(a, false, s), values2<BF16>(a, true, s), values2<BF16>(b, false, s), values2<BF16>(b, true, s));
-        };
-        if (wanted(t)) *reinterpret_cast<uint4*>(k_out + (int64_t)t * D + c) = row8(w[nd].x, w[nd].y);
-        if (wanted(t + 16)) *reinterpret_cast<uint4*>(k_out + (int64_t)(t + 16) * D + c) = row8(w[nd].z, w[nd].w);
-      }
-    }
-    if (P.v_out) {
-      const float s = P.v_scale[block];
-      const bool upper = lane & 8;
-      const int cc = 2 * (lane & 7) + (upper ? 1 : 0);
-      uint4 w[ND];
+      for (int nd = 0; nd < ND; ++nd) k[nd] = *reinterpret_cast<const uint4*>(P.k_codes + slice + nd * 1024 + lane * 16);
+    if (P.v_out)
 #pragma unroll
       for (int nd = 0; nd < ND; ++nd)
-        w[nd] = *reinterpret_cast<const uint4*>(P.v_codes + slice + nd * 1024 + (16 * (lane / 16) + cc) * 16);
+        v[nd] = *reinterpret_cast<const uint4*>(P.v_codes + slice + nd * 1024 + (16 * (lane / 16) + cc) * 16);
+    const float sk = P.k_scale[block], sv = P.v_scale[block];
+    // The rows of a unit are put together in LDS, a wavefront for itself, so that a store covers 1 KB of output in one
+    // stretch: stored from the lanes that convert them (64 bytes of a row at a time, values 4 bytes a lane) 131072 tokens x
+    // 8 heads took 208 us instead of 143.
+    constexpr int PITCH = 2 * D + 16, CHUNKS = D / 8;          // bytes of a row, 16-byte pieces of it
+    __shared__ __align__(16) unsigned char stage[WAVES][32 * PITCH];
+    unsigned char* mine = stage[wave];
+    auto flush = [&](uint16_t* out) {
+      wave_lds_order();
+#pragma unroll
+      for (int x = 0; x < 32 * CHUNKS / 64; ++x) {
+        const int i = lane + 64 * x, t = i / CHUNKS, c = i % CHUNKS;
+        const uint4 y = *reinterpret_cast<const uint4*>(mine + t * PITCH + 16 * c);
+        if (wanted(32 * unit + t)) *reinterpret_cast<uint4*>(out + (int64_t)(32 * unit + t) * D + 8 * c) = y;
+      }
+      wave_lds_order();
+    };
+    if (P.k_out) {
+#pragma unroll
+      for (int nd = 0; nd < ND; ++nd) {
+        const int t = lane % 16, c = 32 * nd + 8 * (lane / 16);
+        auto row8 = [&](uint32_t a, uint32_t b) {
+          return make_uint4(values2<BF16>(a, false, sk), values2<BF16>(a, true, sk), values2<BF16>(b, false, sk), values2<BF16>(b, true, sk));
+        };
+        *reinterpret_cast<uint4*>(mine + t * PITCH + 2 * c) = row8(k[nd].x, k[nd].y);
+        *reinterpret_cast<uint4*>(mine + (t + 16) * PITCH + 2 * c) = row8(k[nd].z, k[nd].w);
+      }
+      flush(k_out);
+    }
+    if (P.v_out) {
 #pragma unroll
       for (int nd = 0; nd < ND; ++nd) {
         // the trade of append8_kernel backwards: the lane is left with channels c, c + 1 of eight tokens
-        const uint32_t got0 = other_half_row(upper ? w[nd].x : w[nd].z), got1 = other_half_row(upper ? w[nd].y : w[nd].w);
-        const uint32_t lo[2] = {upper ? got0 : w[nd].x, upper ? got1 : w[nd].y};
-        const uint32_t hi[2] = {upper ? w[nd].z : got0, upper ? w[nd].w : got1};
+        const uint32_t got0 = other_half_row(upper ? v[nd].x : v[nd].z), got1 = other_half_row(upper ? v[nd].y : v[nd].w);
+        const uint32_t lo[2] = {upper ? got0 : v[nd].x, upper ? got1 : v[nd].y};
+        const uint32_t hi[2] = {upper ? v[nd].z : got0, upper ? v[nd].w : got1};
         const int c = 32 * nd + 2 * (lane % 16);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {
-            const uint32_t x = values2<BF16>(lo[b], e != 0, s), y = values2<BF16>(hi[b], e != 0, s);
-            const int t = 32 * unit + value_token(lane / 16, 4 * b + e);
-            if (wanted(t)) *reinterpret_cast<uint32_t*>(v_out + (int64_t)t * D + c) = __builtin_amdgcn_perm(y, x, 0x05040100);
-            if (wanted(t + 1)) *reinterpret_cast<uint32_t*>(v_out + (int64_t)(t + 1) * D + c) = __builtin_amdgcn_perm(y, x, 0x07060302);
+            const uint32_t x = values2<BF16>(lo[b], e != 0, sv), y = values2<BF16>(hi[b], e != 0, sv);
+            const int t = value_token(lane / 16, 4 * b + e);
+            *reinterpret_cast<uint32_t*>(mine + t * PITCH + 2 * c) = __builtin_amdgcn_perm(y, x, 0x05040100);
+            *reinterpret_cast<uint32_t*>(mine + (t + 1) * PITCH + 2 * c) = __builtin_amdgcn_perm(y, x, 0x07060302);
           }
       }
+      flush(v_out);
     }
     return;
   }
