@@ -1,8 +1,8 @@
 // C ABI of the 8-bit cache: argument checks on the host, then kernel launches.
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
-#include <vector>
 
 #include "lq_cache8.h"
 #include "lq_internal.h"
@@ -43,45 +43,114 @@ static lq_status begin8(const lq_config8* cfg, const lq_cache8* c, Shape8* s) {
   return LQ_OK;
 }
 
-// Rows that are all alike go as one entry.
-static RowArg8 row_arg(const lq_cache8* c, const std::vector<Row8>& rows) {
-  bool same = true;
-  for (const Row8& r : rows) same = same && r.n == rows[0].n && r.x == rows[0].x;
-  return RowArg8{rows.data(), (Row8*)c->seq_state, (int)rows.size(), same};
+// One entry for each batch row: on the stack for the batches that travel in a launch's arguments, else from the heap.
+struct RowList {
+  Row8 few[ROWS_IN_ARGS];
+  Row8* many = nullptr;
+  Row8* e;
+  int n;
+  explicit RowList(int rows) : e(few), n(rows) {
+    if (n > ROWS_IN_ARGS) e = many = static_cast<Row8*>(malloc(n * sizeof(Row8)));
+  }
+  ~RowList() { free(many); }
+  RowList(const RowList&) = delete;
+  bool ok() const { return e != nullptr; }
+  bool alike() const {
+    for (int b = 1; b < n; ++b)
+      if (e[b].n != e[0].n || e[b].x != e[0].x) return false;
+    return true;
+  }
+  RowArg8 arg(const lq_cache8* c, bool same) const { return RowArg8{e, (Row8*)c->seq_state, n, same}; }
+};
+
+// Parts of a row's items when none may be larger than `most`.
+static int parts_of(const Shape8& s, const Row8& r, int64_t most) {
+  const int64_t u = units8(r.n, s.G);
+  return u > most ? (int)((u + most - 1) / most) : 1;
 }
 
-// Fills the rows' parts, first workgroups and order.  256 workgroups of 4 wavefronts read as fast as the memory delivers;
-// an item is split into parts of a 256th of all work (8 units at least, two to a wavefront), unless it is less than a 128th:
-// then its share of the time is smaller than what a join costs.
-static void plan8(const Shape8& s, bool same, std::vector<Row8>* rows, Plan8* p) {
+// Fills the rows' parts, order and first workgroups, and says whether the rows still are alike.
+//
+// A compute unit reads up to 1.5 times its share of the memory's rate, so a launch is as fast as the memory where no compute
+// unit has much more than a 256th of the work, and 256 workgroups, of 4 wavefronts already, are placed one to a compute unit.
+// Times in us, d = 128, 4 heads a kv head, before (items whole, or in parts of a 256th rounded up) and with each rule:
+//  - items that are fewer: as many parts each as make up to 256 workgroups (24 items of 16384 tokens: 11 parts, 264
+//    workgroups, 25.7; 10 parts 20.6), none of less than 8 units, two to a wavefront.
+//  - between 128 and 256 items that cannot be split evenly stay whole, up to 200 of them in workgroups of 8 wavefronts, which
+//    use that reserve (132 items of 4096 tokens: 4 wavefronts 31.3, 8 27.7; 180 items 34.3 and 34.6).
+//  - a few items more than 256: rows for 256 stay whole, the rest is split into 256 (260 items 59.5 -> 50.9; 304 items
+//    64.4 -> 56.9; from 340 on the reserve covers the second item of a compute unit).
+// Rows of different lengths:
+//  - up to 256 items: the smallest `most` that makes no more than 256 parts (16 rows of up to 8000 x 8 kv heads 36.1 -> 31.9;
+//    4 rows of up to 30000 34.8 -> 28.7), if that is within 1.5 of the even share.
+//  - else what is over a 200th of all work is split into parts of a 256th, and few and large workgroups, of 8 or 16
+//    wavefronts, the longest first, leave the balance to their placement (64 rows of up to 4096 x 8 kv heads: 4 wavefronts
+//    54.5, 8 54.6, 16 49.5; 100 of up to 4000: 79.9, 75.8, 76.4; 30 of up to 9000, d = 96: 43.0, 43.6, 47.0), unless they are
+//    small (200 rows of up to 2000, 31 units each: 4 wavefronts 75.6, 16 84.6) or many, which balance by their number.
+static bool plan8(const Shape8& s, bool same, RowList* rows, Plan8* p) {
+  constexpr int CUS = 256, LEAST = 8;
   p->groups = head_groups8(s);
   p->hb = (s.gh + p->groups - 1) / p->groups;
   p->waves = 4;
   const int per_row = s.Hkv * p->groups;
-  int64_t work = 0;
-  for (const Row8& r : *rows) work += units8(r.n, s.G);
-  work *= per_row;
-  const int64_t most = std::max<int64_t>((work + 255) / 256, 8);
-  if (!same) std::sort(rows->begin(), rows->end(), [](const Row8& x, const Row8& y) { return x.n > y.n; });
-  int x = 0;
-  for (Row8& r : *rows) {
-    const int64_t u = units8(r.n, s.G);
-    r.parts = u * 128 <= work ? 1 : (int)std::max<int64_t>((u + most - 1) / most, 1);
-    r.x = x;
-    x += r.parts * per_row;
+  const int64_t items = (int64_t)s.B * per_row;
+  Row8 *first = rows->e, *last = rows->e + rows->n;
+  if (same) {
+    const int u = units8(first->n, s.G), most_parts = std::max(u / LEAST, 1);
+    const int parts = items <= CUS / 2 ? std::min((int)(CUS / items), most_parts) : 1;
+    for (Row8* r = first; r != last; ++r) r->parts = parts;
+    if (items > CUS / 2 && items <= 200) p->waves = 8;
+    if (items > CUS && items < 340 && per_row <= CUS) {
+      const int left = s.B - CUS / per_row;
+      const int split = std::min(CUS / (left * per_row), most_parts);
+      if (split > 1) {
+        for (Row8* r = first; r != first + left; ++r) r->parts = split;
+        same = false;
+      }
+    }
+  } else {
+    int64_t work = 0, longest = LEAST, most = 0;
+    for (Row8* r = first; r != last; ++r) {
+      const int64_t u = units8(r->n, s.G);
+      work += u * per_row;
+      longest = std::max(longest, u);
+    }
+    if (items <= CUS) {
+      int64_t lo = LEAST, hi = longest;
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        int64_t n = 0;
+        for (Row8* r = first; r != last; ++r) n += parts_of(s, *r, mid);
+        if (n * per_row <= CUS) hi = mid; else lo = mid + 1;
+      }
+      if (lo == LEAST || 2 * lo * CUS <= 3 * work) most = lo;
+    }
+    if (most) {
+      for (Row8* r = first; r != last; ++r) r->parts = parts_of(s, *r, most);
+    } else {
+      most = std::max<int64_t>((work + CUS - 1) / CUS, LEAST);
+      for (Row8* r = first; r != last; ++r) r->parts = units8(r->n, s.G) * 200ll <= work ? 1 : parts_of(s, *r, most);
+      if (items <= 1024 && work >= 24 * items) p->waves = items < CUS ? 8 : 16;
+    }
+    // (by work, not by tokens: what is split has to come first)
+    std::sort(first, last, [&s](const Row8& x, const Row8& y) { return units8(x.n, s.G) > units8(y.n, s.G); });
   }
-  p->blocks = x;
+  while (p->waves * partial_floats8(p->hb, s.d) * (int)sizeof(float) > 65536) p->waves /= 2;   // LDS that a launch may ask for
+  p->blocks = 0;
+  for (Row8* r = first; r != last; ++r) {
+    r->x = p->blocks;
+    p->blocks += r->parts * per_row;
+  }
+  return same;
 }
 
-static lq_status attend8(const Shape8& s, const lq_cache8& c, std::vector<Row8>* rows, const void* k_new, const void* v_new,
-                         const void* q, float softmax_scale, void* out, void* workspace, hipStream_t stream) {
-  bool same = true;
-  for (const Row8& r : *rows) same = same && r.n == (*rows)[0].n;
+static lq_status attend8(const Shape8& s, const lq_cache8& c, RowList* rows, const void* k_new, const void* v_new, const void* q,
+                         float softmax_scale, void* out, void* workspace, hipStream_t stream) {
   Plan8 plan;
-  plan8(s, same, rows, &plan);
+  const bool same = plan8(s, rows->alike(), rows, &plan);
   if (!(softmax_scale > 0.f)) softmax_scale = 1.0f / sqrtf((float)s.d);
-  RowArg8 arg{rows->data(), (Row8*)c.seq_state, (int)rows->size(), same};
-  return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, arg, stream) == hipSuccess ? LQ_OK : LQ_ERR_HIP;
+  return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, rows->arg(&c, same), stream) == hipSuccess ? LQ_OK
+                                                                                                                             : LQ_ERR_HIP;
 }
 
 extern "C" {
@@ -118,13 +187,14 @@ lq_status logquant_append8(const lq_config8* cfg, lq_cache8* cache, const void* 
   const lq_status st = begin8(cfg, cache, &s);
   if (st != LQ_OK) return st;
   if (n_max < 1 || !aligned16(k_new) || !aligned16(v_new)) return LQ_ERR_SHAPE;
-  std::vector<Row8> rows(s.B);
+  RowList rows(s.B);
+  if (!rows.ok()) return LQ_ERR_CAPACITY;
   int blocks = 0;
   for (int b = 0; b < s.B; ++b) {
     const int take = n_new ? n_new[b] : n_max;
     if (take < 0 || take > n_max) return LQ_ERR_SHAPE;
     if (take > s.cap - cache->n[b]) return LQ_ERR_CAPACITY;
-    rows[b] = Row8{cache->n[b], take, 1, b};
+    rows.e[b] = Row8{cache->n[b], take, 1, b};
     // a workgroup for each block that becomes full, and one for the rest, unless the first has rows in the tail (append8_kernel)
     const int held = cache->n[b] % s.G, full = (held + take) / s.G, rest = (held + take) % s.G;
     const int need = !take ? 0 : full + (rest && !(held && full) ? 1 : 0);
@@ -132,8 +202,8 @@ lq_status logquant_append8(const lq_config8* cfg, lq_cache8* cache, const void* 
   }
   if (!blocks) return LQ_OK;   // nobody takes a token
   clear_stale_error();
-  if (launch_append8(s, *cache, k_new, v_new, n_max, blocks, row_arg(cache, rows), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
-  for (int b = 0; b < s.B; ++b) cache->n[b] += rows[b].x;
+  if (launch_append8(s, *cache, k_new, v_new, n_max, blocks, rows.arg(cache, rows.alike()), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
+  for (int b = 0; b < s.B; ++b) cache->n[b] += rows.e[b].x;
   return LQ_OK;
 }
 
@@ -143,15 +213,16 @@ lq_status logquant_read8(const lq_config8* cfg, const lq_cache8* cache, int32_t 
   const lq_status st = begin8(cfg, cache, &s);
   if (st != LQ_OK) return st;
   if (t0 < 0 || n < 1 || t0 > s.cap || n > s.cap - t0 || !aligned16(k_out) || !aligned16(v_out)) return LQ_ERR_SHAPE;
-  std::vector<Row8> rows(s.B);
+  RowList rows(s.B);
+  if (!rows.ok()) return LQ_ERR_CAPACITY;
   int longest = 0;
   for (int b = 0; b < s.B; ++b) {
-    rows[b] = Row8{cache->n[b], 0, 1, b};
+    rows.e[b] = Row8{cache->n[b], 0, 1, b};
     if (cache->n[b] > longest) longest = cache->n[b];
   }
   if (longest <= t0) return LQ_OK;   // nothing of the range is there
   clear_stale_error();
-  return launch_read8(s, *cache, t0, n, k_out, v_out, row_arg(cache, rows), (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_HIP;
+  return launch_read8(s, *cache, t0, n, k_out, v_out, rows.arg(cache, rows.alike()), (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_HIP;
 }
 
 lq_status logquant_decode_attn8(const lq_config8* cfg, const lq_cache8* cache, const void* q, float softmax_scale, void* out,
@@ -161,8 +232,9 @@ lq_status logquant_decode_attn8(const lq_config8* cfg, const lq_cache8* cache, c
   const lq_status st = begin8(cfg, cache, &s);
   if (st != LQ_OK) return st;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return LQ_ERR_SHAPE;
-  std::vector<Row8> rows(s.B);
-  for (int b = 0; b < s.B; ++b) rows[b] = Row8{cache->n[b], 0, 1, b};
+  RowList rows(s.B);
+  if (!rows.ok()) return LQ_ERR_CAPACITY;
+  for (int b = 0; b < s.B; ++b) rows.e[b] = Row8{cache->n[b], 0, 1, b};
   clear_stale_error();
   return attend8(s, *cache, &rows, nullptr, nullptr, q, softmax_scale, out, workspace, (hipStream_t)stream);
 }
@@ -174,18 +246,20 @@ lq_status logquant_decode_step8(const lq_config8* cfg, lq_cache8* cache, const v
   lq_status st = begin8(cfg, cache, &s);
   if (st != LQ_OK) return st;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return LQ_ERR_SHAPE;
-  std::vector<Row8> rows(s.B);
+  RowList rows(s.B);
+  if (!rows.ok()) return LQ_ERR_CAPACITY;
   bool fills = false;
   for (int b = 0; b < s.B; ++b) {
     if (cache->n[b] == s.cap) return LQ_ERR_CAPACITY;
-    rows[b] = Row8{cache->n[b] + 1, 0, 1, b};
-    fills = fills || rows[b].n % s.G == 0;
+    rows.e[b] = Row8{cache->n[b] + 1, 0, 1, b};
+    fills = fills || rows.e[b].n % s.G == 0;
   }
   clear_stale_error();
   if (fills) {   // a block has to be quantized before it is attended to
-    std::vector<Row8> one(s.B);
-    for (int b = 0; b < s.B; ++b) one[b] = Row8{cache->n[b], 1, 1, b};
-    if (launch_append8(s, *cache, k_new, v_new, 1, 1, row_arg(cache, one), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
+    RowList one(s.B);
+    if (!one.ok()) return LQ_ERR_CAPACITY;
+    for (int b = 0; b < s.B; ++b) one.e[b] = Row8{cache->n[b], 1, 1, b};
+    if (launch_append8(s, *cache, k_new, v_new, 1, 1, one.arg(cache, one.alike()), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
     k_new = v_new = nullptr;
   }
   st = attend8(s, *cache, &rows, k_new, v_new, q, softmax_scale, out, workspace, (hipStream_t)stream);

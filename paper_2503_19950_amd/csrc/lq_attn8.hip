@@ -156,35 +156,44 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
     for (int nd = 0; nd < ND; ++nd) q[nd] = load16(rs, head * D * 2 + a * 16 + nd * 64);
   }
 
-  // Units of the tail that are ours go to the last wavefronts, one each, which sit out the first two rounds of codes.
+  // Units of the tail that are ours go to the first wavefronts, one each, which sit out two rounds of codes for it: they are
+  // the oldest, and their loads are served first.
   int tails = 0;
   for (int i = 0; 32 * i < rest; ++i) tails += codes + 2 * i >= pos && codes + 2 * i < to;
   const int skip = pos > codes ? (pos - codes + 1) / 2 : 0;               // units of the tail before ours
-  const int tail_unit = skip + NW - 1 - wave;
-  const bool has_tail = NW - 1 - wave < tails;
+  const int tail_unit = skip + wave;
+  const bool has_tail = wave < tails;
   const int workers = tails < NW ? NW - tails : NW;                       // wavefronts in the first two rounds
   const int stop = to < codes ? to : codes;
-  int i = pos + (wave < workers ? wave : wave + 2 * workers), round = wave < workers ? 0 : 2;
+  const bool sits_out = has_tail && workers < NW;
+  int i = pos + (sits_out ? wave + 2 * workers : wave - (NW - workers)), step = sits_out ? NW : workers;
 
   const __amdgpu_buffer_rsrc_t rk = buffer(P.k_codes + bh * P.cap * D, stop * UNIT);   // behind the last unit: zeros, no reads
   const __amdgpu_buffer_rsrc_t rv = buffer(P.v_codes + bh * P.cap * D, stop * UNIT);
   typedef const float __attribute__((address_space(4))) * ScalePtr;      // read by scalar loads
   const ScalePtr ks = (ScalePtr)(uintptr_t)(P.k_scale + bh * (P.cap >> P.log_g));
   const ScalePtr vs = (ScalePtr)(uintptr_t)(P.v_scale + bh * (P.cap >> P.log_g));
+  // Workgroups begin somewhere in their part and go round.  All from the front, those of a launch would be at the same
+  // distance into their slices all along, and with some capacities, whose slices lie a multiple of the memory's interleaving
+  // apart, wait for the same few channels: 8 kv heads of 131072 tokens in slices of 132096 82.9 instead of 49.1 us, 64 rows
+  // of 2048 in slices of 4128 55.3 instead of 47.0 (in slices of 4160 46.4 either way).
+  const int len = stop - pos;
+  const int turn = len > 0 ? (int)((uint64_t)(blockIdx.x * 0x9E3779B1u) * (uint32_t)len >> 32) : 0;
   u32x4 k[ND], v[ND];
   float ck, cv;
+  int unit;                                            // the i-th of the part, counted from there; behind the last: `stop`
   auto load_k = [&]() {
+    unit = i + turn < stop ? i + turn : i + turn - len;
+    if (i >= stop) unit = stop;
 #pragma unroll
-    for (int nd = 0; nd < ND; ++nd) k[nd] = load16(rk, i * UNIT + lane * 16 + nd * 1024);
+    for (int nd = 0; nd < ND; ++nd) k[nd] = load16(rk, unit * UNIT + lane * 16 + nd * 1024);
+    const int block = i < stop ? unit >> (P.log_g - 5) : 0;
+    ck = ks[block];
+    cv = vs[block];
   };
   auto load_v = [&]() {
 #pragma unroll
-    for (int nd = 0; nd < ND; ++nd) v[nd] = load16(rv, i * UNIT + lane * 16 + nd * 1024);
-  };
-  auto load_scales = [&]() {
-    const int block = i < stop ? i >> (P.log_g - 5) : 0;
-    ck = ks[block];
-    cv = vs[block];
+    for (int nd = 0; nd < ND; ++nd) v[nd] = load16(rv, unit * UNIT + lane * 16 + nd * 1024);
   };
 
   f32x4 acc[NT];
@@ -208,11 +217,14 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
     const int left = rest - 32 * tail_unit, live = left < 32 ? left : 32;
     uint16_t* k_tail = P.k_tail + (bh << P.log_g) * D;
     uint16_t* v_tail = P.v_tail + (bh << P.log_g) * D;
+    // lanes whose rows are not there read nothing
+    const __amdgpu_buffer_rsrc_t rkt = buffer(k_tail + 32 * tail_unit * D, 64 * D), rvt = buffer(v_tail + 32 * tail_unit * D, 64 * D);
+    const int nothing = 64 * D;
     u32x4 kt[2 * ND], vt[NT];
 #pragma unroll
-    for (int t = 0; t < 2 * ND; ++t) kt[t] = *reinterpret_cast<const u32x4*>(k_tail + 32 * tail_unit * D + (t * 64 + lane) * 8);
+    for (int t = 0; t < 2 * ND; ++t) kt[t] = load16(rkt, 16 * (t / ND) + head < live ? t * 1024 + lane * 16 : nothing);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) vt[t] = *reinterpret_cast<const u32x4*>(v_tail + 32 * tail_unit * D + (t * 64 + lane) * 8);
+    for (int t = 0; t < NT; ++t) vt[t] = load16(rvt, 4 * a < live ? t * 1024 + lane * 16 : nothing);
     if constexpr (STEP) {                            // the new row takes its place, here and (every head group) in the cache
       if (left <= 32) {
         const int t = left - 1, r = 32 * tail_unit + t, e = 4 * (t / 16) + t % 4;
@@ -280,7 +292,6 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
   // ---- codes; the keys of the next unit are under way while the values of this one are used
   if (i < stop) {
     load_k();
-    load_scales();
     load_v();
   }
   while (i < stop) {
@@ -291,10 +302,9 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
       s1 = mfma<BF16>(codes_as<BF16>(k[nd][2], k[nd][3]), q[nd], s1);
     }
     const float c = ck * P.scale, f = cv;
-    i += round < 2 ? workers : NW;
-    ++round;
+    i += step;
+    step = NW;
     load_k();
-    load_scales();
     look_up(fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3]))) * c);
     float p[8];
 #pragma unroll
@@ -444,6 +454,8 @@ hipError_t attn8(const Shape8& s, const Attn8Params& p, const Rows8<MODE>& rows,
     go(attn8_kernel<T, 128, NW, MODE, STEP>);
   };
   auto with_type = [&](auto bf16) {
+    if (plan.waves == 16) return with_waves(bf16, std::integral_constant<int, 16>{});
+    if (plan.waves == 8) return with_waves(bf16, std::integral_constant<int, 8>{});
     with_waves(bf16, std::integral_constant<int, 4>{});
   };
   if (s.bf16) with_type(std::true_type{}); else with_type(std::false_type{});

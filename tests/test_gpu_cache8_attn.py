@@ -66,6 +66,57 @@ def test_more_rows_than_travel_in_a_launch():
     U.check_output(out, q, oracle, "f16")
 
 
+def shapes_of_plans():
+    """Numbers of items around those where the workgroups' plan changes, with rows alike and not, and rows whose work
+    is not in the order of their lengths (a tail of 127 tokens counts more than the block that it becomes)."""
+    frac = lambda B, L: [L - int(L * (b * 0.6180339887 % 1.0)) for b in range(B)]  # noqa: E731
+    return [
+        ("few_alike", 3, 2, 64, [3000] * 3), ("half_alike", 33, 4, 32, [400] * 33), ("nearly_full_alike", 60, 4, 32, [300] * 60),
+        ("one_more_alike", 65, 4, 32, [700] * 65), ("more_alike", 85, 4, 32, [300] * 85), ("many_alike", 130, 4, 32, [100] * 130),
+        ("few", 9, 4, 64, frac(9, 6000)), ("nearly_full", 62, 4, 32, frac(62, 1500)), ("one_long", 66, 4, 32, [9000] + [65] * 65),
+        ("one_long_few", 20, 4, 32, [9000] + [65] * 19), ("large", 70, 4, 64, frac(70, 2500)), ("many", 280, 4, 32, frac(280, 300)),
+        ("tails", 300, 4, 128, [(i % 2) * 127 + 128 * (1 + (i + 1) % 2) for i in range(300)]),
+        ("long_and_tails", 150, 2, 128, [12000, 11999, 11904] + [(i % 2) * 127 + 128 * (1 + (i + 1) % 2) for i in range(147)]),
+    ]
+
+
+@pytest.mark.parametrize("name,B,Hkv,G,lengths", shapes_of_plans(), ids=[x[0] for x in shapes_of_plans()])
+def test_shapes_of_plans(name, B, Hkv, G, lengths):
+    cache, oracle = build(301, B, 2 * Hkv, Hkv, 64, G, "f16", lengths)
+    q = queries(302, B, 2 * Hkv, 64, "f16").to(U.DEVICE)
+    out = cache.decode_attn(q, torch.full_like(q, float("nan")))
+    U.check_output(out, q.cpu(), oracle, "f16", rows_of=sorted(set(list(range(0, B, max(1, B // 12))) + [0, 1, 2, B - 2, B - 1])))
+    assert torch.isfinite(out).all()
+    assert torch.equal(cache.decode_attn(q), out)
+
+
+@pytest.mark.parametrize("dtype,gh,lengths", [("bf16", 16, [3000 - 37 * i for i in range(40)]), ("f16", 7, [3000 - 37 * i for i in range(40)]),
+                                              ("f16", 15, [3000 - 37 * i for i in range(40)]), ("bf16", 16, [500] * 20)])
+def test_many_heads_in_large_workgroups(dtype, gh, lengths):
+    """Head counts at which a workgroup's merge outgrows what a launch may ask of LDS, with 8 kv heads and d = 128."""
+    B = len(lengths)
+    cache, oracle = build(311, B, 8 * gh, 8, 128, 32, dtype, lengths)
+    q = queries(312, B, 8 * gh, 128, dtype)
+    U.check_output(cache.decode_attn(q.to(U.DEVICE)), q, oracle, dtype, rows_of=[0, 1, B // 2, B - 1])
+
+
+def test_counts_set_back_within_a_block():
+    """Tokens that are dropped again: within the tail, and from a block that single tokens have just filled."""
+    G, d = 64, 64
+    cache, oracle = build(321, 2, 2, 1, d, G, "f16", [G - 3, 2 * G - 3], capacity=4 * G)
+    held = [cache.clone()]
+    steps = [(U.rows(330 + i, 2, 1, 1, d, "f16").to(U.DEVICE), U.rows(340 + i, 2, 1, 1, d, "f16").to(U.DEVICE)) for i in range(3)]
+    for k, v in steps:
+        cache.append(k, v)
+        held.append(cache.clone())
+    q = queries(351, 2, 2, d, "f16").to(U.DEVICE)
+    for back in (1, 2, 3):
+        cache.set_counts([G - back, 2 * G - back])
+        assert torch.equal(cache.decode_attn(q), held[3 - back].decode_attn(q))
+    cache.set_counts([G - 3, 2 * G - 3])
+    oracle.check(cache)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("scale", [0.0, 0.3, 1e-3])
 def test_scales_of_the_softmax(dtype, scale):
