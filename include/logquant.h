@@ -409,8 +409,8 @@ lq_status logquant_decode_attn8(const lq_config8 *cfg, const lq_cache8 *cache, c
                                 float softmax_scale, void *out, void *workspace, void *stream);
 
 /* One decode step: logquant_append8 of one token for every row, then logquant_decode_attn8
- * over the cache including it, with the results of the two calls.  One launch when no
- * row's block becomes full, else two.
+ * over the cache including it, in one launch, with the results of the two calls (outputs up
+ * to the order of fp32 sums).
  *   k_new, v_new : DEVICE [B][Hkv][1][d] T.  LQ_ERR_CAPACITY if a row is full. */
 lq_status logquant_decode_step8(const lq_config8 *cfg, lq_cache8 *cache, const void *k_new,
                                 const void *v_new, const void *q, float softmax_scale, void *out,

@@ -63,11 +63,10 @@ struct RowList {
   RowArg8 arg(const lq_cache8* c, bool same) const { return RowArg8{e, (Row8*)c->seq_state, n, same}; }
 };
 
-// Parts of a row's items when none may be larger than `most`.
-static int parts_of(const Shape8& s, const Row8& r, int64_t most) {
-  const int64_t u = units8(r.n, s.G);
-  return u > most ? (int)((u + most - 1) / most) : 1;
-}
+// Parts of an item of u units when none may be larger than `most`.  Up to 20 units, five to a wavefront, it stays whole
+// (512 tokens x 8 kv heads: whole 4.9 us, 2 parts 6.4, 4 parts 6.0; 1024 tokens: 6.9, 7.2, 6.4 and 8 parts 5.8).
+constexpr int WHOLE = 20;
+static int parts_of(int64_t u, int64_t most) { return u > most && u > WHOLE ? (int)((u + most - 1) / most) : 1; }
 
 // Fills the rows' parts, order and first workgroups, and says whether the rows still are alike.
 //
@@ -75,7 +74,7 @@ static int parts_of(const Shape8& s, const Row8& r, int64_t most) {
 // unit has much more than a 256th of the work, and 256 workgroups, of 4 wavefronts already, are placed one to a compute unit.
 // Times in us, d = 128, 4 heads a kv head, before (items whole, or in parts of a 256th rounded up) and with each rule:
 //  - items that are fewer: as many parts each as make up to 256 workgroups (24 items of 16384 tokens: 11 parts, 264
-//    workgroups, 25.7; 10 parts 20.6), none of less than 8 units, two to a wavefront.
+//    workgroups, 25.7; 10 parts 20.6), none of less than 4 units, one to a wavefront.
 //  - between 128 and 256 items that cannot be split evenly stay whole, up to 200 of them in workgroups of 8 wavefronts, which
 //    use that reserve (132 items of 4096 tokens: 4 wavefronts 31.3, 8 27.7; 180 items 34.3 and 34.6).
 //  - a few items more than 256: rows for 256 stay whole, the rest is split into 256 (260 items 59.5 -> 50.9; 304 items
@@ -87,8 +86,9 @@ static int parts_of(const Shape8& s, const Row8& r, int64_t most) {
 //    wavefronts, the longest first, leave the balance to their placement (64 rows of up to 4096 x 8 kv heads: 4 wavefronts
 //    54.5, 8 54.6, 16 49.5; 100 of up to 4000: 79.9, 75.8, 76.4; 30 of up to 9000, d = 96: 43.0, 43.6, 47.0), unless they are
 //    small (200 rows of up to 2000, 31 units each: 4 wavefronts 75.6, 16 84.6) or many, which balance by their number.
-static bool plan8(const Shape8& s, bool same, RowList* rows, Plan8* p) {
-  constexpr int CUS = 256, LEAST = 8;
+static bool plan8(const Shape8& s, bool same, bool step, RowList* rows, Plan8* p) {
+  constexpr int CUS = 256, LEAST = 4;
+  auto units = [&](const Row8& r) -> int64_t { return units8(r.n, s.G, step); };
   p->groups = head_groups8(s);
   p->hb = (s.gh + p->groups - 1) / p->groups;
   p->waves = 4;
@@ -96,7 +96,7 @@ static bool plan8(const Shape8& s, bool same, RowList* rows, Plan8* p) {
   const int64_t items = (int64_t)s.B * per_row;
   Row8 *first = rows->e, *last = rows->e + rows->n;
   if (same) {
-    const int u = units8(first->n, s.G), most_parts = std::max(u / LEAST, 1);
+    const int u = (int)units(*first), most_parts = u > WHOLE ? u / LEAST : 1;
     const int parts = items <= CUS / 2 ? std::min((int)(CUS / items), most_parts) : 1;
     for (Row8* r = first; r != last; ++r) r->parts = parts;
     if (items > CUS / 2 && items <= 200) p->waves = 8;
@@ -111,7 +111,7 @@ static bool plan8(const Shape8& s, bool same, RowList* rows, Plan8* p) {
   } else {
     int64_t work = 0, longest = LEAST, most = 0;
     for (Row8* r = first; r != last; ++r) {
-      const int64_t u = units8(r->n, s.G);
+      const int64_t u = units(*r);
       work += u * per_row;
       longest = std::max(longest, u);
     }
@@ -120,20 +120,20 @@ static bool plan8(const Shape8& s, bool same, RowList* rows, Plan8* p) {
       while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;
         int64_t n = 0;
-        for (Row8* r = first; r != last; ++r) n += parts_of(s, *r, mid);
+        for (Row8* r = first; r != last; ++r) n += parts_of(units(*r), mid);
         if (n * per_row <= CUS) hi = mid; else lo = mid + 1;
       }
       if (lo == LEAST || 2 * lo * CUS <= 3 * work) most = lo;
     }
     if (most) {
-      for (Row8* r = first; r != last; ++r) r->parts = parts_of(s, *r, most);
+      for (Row8* r = first; r != last; ++r) r->parts = parts_of(units(*r), most);
     } else {
       most = std::max<int64_t>((work + CUS - 1) / CUS, LEAST);
-      for (Row8* r = first; r != last; ++r) r->parts = units8(r->n, s.G) * 200ll <= work ? 1 : parts_of(s, *r, most);
+      for (Row8* r = first; r != last; ++r) r->parts = units(*r) * 200 <= work ? 1 : parts_of(units(*r), most);
       if (items <= 1024 && work >= 24 * items) p->waves = items < CUS ? 8 : 16;
     }
     // (by work, not by tokens: what is split has to come first)
-    std::sort(first, last, [&s](const Row8& x, const Row8& y) { return units8(x.n, s.G) > units8(y.n, s.G); });
+    std::sort(first, last, [&](const Row8& x, const Row8& y) { return units(x) > units(y); });
   }
   while (p->waves * partial_floats8(p->hb, s.d) * (int)sizeof(float) > 65536) p->waves /= 2;   // LDS that a launch may ask for
   p->blocks = 0;
@@ -147,7 +147,7 @@ static bool plan8(const Shape8& s, bool same, RowList* rows, Plan8* p) {
 static lq_status attend8(const Shape8& s, const lq_cache8& c, RowList* rows, const void* k_new, const void* v_new, const void* q,
                          float softmax_scale, void* out, void* workspace, hipStream_t stream) {
   Plan8 plan;
-  const bool same = plan8(s, rows->alike(), rows, &plan);
+  const bool same = plan8(s, rows->alike(), k_new != nullptr, rows, &plan);
   if (!(softmax_scale > 0.f)) softmax_scale = 1.0f / sqrtf((float)s.d);
   return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, rows->arg(&c, same), stream) == hipSuccess ? LQ_OK
                                                                                                                              : LQ_ERR_HIP;
@@ -248,20 +248,11 @@ lq_status logquant_decode_step8(const lq_config8* cfg, lq_cache8* cache, const v
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return LQ_ERR_SHAPE;
   RowList rows(s.B);
   if (!rows.ok()) return LQ_ERR_CAPACITY;
-  bool fills = false;
   for (int b = 0; b < s.B; ++b) {
     if (cache->n[b] == s.cap) return LQ_ERR_CAPACITY;
     rows.e[b] = Row8{cache->n[b] + 1, 0, 1, b};
-    fills = fills || rows.e[b].n % s.G == 0;
   }
   clear_stale_error();
-  if (fills) {   // a block has to be quantized before it is attended to
-    RowList one(s.B);
-    if (!one.ok()) return LQ_ERR_CAPACITY;
-    for (int b = 0; b < s.B; ++b) one.e[b] = Row8{cache->n[b], 1, 1, b};
-    if (launch_append8(s, *cache, k_new, v_new, 1, 1, one.arg(cache, one.alike()), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
-    k_new = v_new = nullptr;
-  }
   st = attend8(s, *cache, &rows, k_new, v_new, q, softmax_scale, out, workspace, (hipStream_t)stream);
   if (st == LQ_OK)
     for (int b = 0; b < s.B; ++b) cache->n[b] += 1;

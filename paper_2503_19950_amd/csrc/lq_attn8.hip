@@ -19,6 +19,7 @@
 #include "lq_cache8.h"
 #include "lq_device.h"
 #include "lq_internal.h"
+#include "lq_quant8.h"
 
 namespace lq {
 
@@ -39,10 +40,10 @@ constexpr int DEVICE_COHERENT = 16;          // cache policy of partial results:
 struct Attn8Params {
   const uint16_t* q;
   uint16_t* out;
-  const uint8_t *k_codes, *v_codes;
-  const float *k_scale, *v_scale;
+  uint8_t *k_codes, *v_codes;                // (written by a step whose token fills up a block)
+  float *k_scale, *v_scale;
   uint16_t *k_tail, *v_tail;
-  const uint16_t *k_new, *v_new;             // fused step: the token that belongs to the last row of the tail; else null
+  const uint16_t *k_new, *v_new;             // step: the token that becomes the last row of the tail; else null
   int* counters;
   float* partials;
   const Row8* rows;
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
     local = blockIdx.x - mine.x;
   }
   const int j = local / parts, part = local - j * parts;
-  const int codes = n >> P.log_g << (P.log_g - 5), rest = n - 32 * codes;   // units of codes, rows of the tail
+  const int codes = (STEP ? n - 1 : n) >> P.log_g << (P.log_g - 5), rest = n - 32 * codes;   // units of codes, rows of the tail
   const int work = codes + 2 * ((rest + 31) / 32), size = (work + parts - 1) / parts;
   const int pos = part * size, to = pos + size < work ? pos + size : work;
   const int h = j / P.groups, g = j - h * P.groups;
@@ -156,12 +157,9 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
     for (int nd = 0; nd < ND; ++nd) q[nd] = load16(rs, head * D * 2 + a * 16 + nd * 64);
   }
 
-  // Units of the tail that are ours go to the first wavefronts, one each, which sit out two rounds of codes for it: they are
-  // the oldest, and their loads are served first.
-  int tails = 0;
-  for (int i = 0; 32 * i < rest; ++i) tails += codes + 2 * i >= pos && codes + 2 * i < to;
-  const int skip = pos > codes ? (pos - codes + 1) / 2 : 0;               // units of the tail before ours
-  const int tail_unit = skip + wave;
+  // The tail belongs to the last part.  Its units go to the first wavefronts, one each, which sit out two rounds of codes for
+  // it: they are the oldest, and their loads are served first.
+  const int tails = part == parts - 1 ? (rest + 31) / 32 : 0;
   const bool has_tail = wave < tails;
   const int workers = tails < NW ? NW - tails : NW;                       // wavefronts in the first two rounds
   const int stop = to < codes ? to : codes;
@@ -213,21 +211,22 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
   };
 
   // ---- rows of the tail
-  if (has_tail) {
-    const int left = rest - 32 * tail_unit, live = left < 32 ? left : 32;
+  bool ready = false;                                  // k, v hold codes that are not in memory yet
+  if (tails) {
     uint16_t* k_tail = P.k_tail + (bh << P.log_g) * D;
     uint16_t* v_tail = P.v_tail + (bh << P.log_g) * D;
-    // lanes whose rows are not there read nothing
-    const __amdgpu_buffer_rsrc_t rkt = buffer(k_tail + 32 * tail_unit * D, 64 * D), rvt = buffer(v_tail + 32 * tail_unit * D, 64 * D);
-    const int nothing = 64 * D;
+    const int left = rest - 32 * wave, live = left < 32 ? left : 32;
     u32x4 kt[2 * ND], vt[NT];
+    if (has_tail) {
+      // lanes whose rows are not there read nothing
+      const __amdgpu_buffer_rsrc_t rkt = buffer(k_tail + 32 * wave * D, 64 * D), rvt = buffer(v_tail + 32 * wave * D, 64 * D);
+      const int nothing = 64 * D;
 #pragma unroll
-    for (int t = 0; t < 2 * ND; ++t) kt[t] = load16(rkt, 16 * (t / ND) + head < live ? t * 1024 + lane * 16 : nothing);
+      for (int t = 0; t < 2 * ND; ++t) kt[t] = load16(rkt, 16 * (t / ND) + head < live ? t * 1024 + lane * 16 : nothing);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) vt[t] = load16(rvt, 4 * a < live ? t * 1024 + lane * 16 : nothing);
-    if constexpr (STEP) {                            // the new row takes its place, here and (every head group) in the cache
-      if (left <= 32) {
-        const int t = left - 1, r = 32 * tail_unit + t, e = 4 * (t / 16) + t % 4;
+      for (int t = 0; t < NT; ++t) vt[t] = load16(rvt, 4 * a < live ? t * 1024 + lane * 16 : nothing);
+      if (STEP && left <= 32) {                        // the new row takes its place, here and (every head group) in the cache
+        const int t = left - 1, r = 32 * wave + t, e = 4 * (t / 16) + t % 4;
         u32x4 k_new[ND];
         uint16_t v_new[NT];
 #pragma unroll
@@ -253,48 +252,96 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
         }
       }
     }
-    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+    if (STEP && rest >> P.log_g) {
+      // The new row fills up the block: quantized here as append8_kernel does it (operands of the tail and pieces of codes
+      // have the same tokens and channels in a lane), and attended to as codes.
+      __shared__ uint32_t tops[4];
+      uint32_t top = 0;
+      if (has_tail) {
+        uint32_t top_k = 0, top_v = 0;
 #pragma unroll
-    for (int nd = 0; nd < ND; ++nd) {
-      s0 = mfma<BF16>(kt[nd], q[nd], s0);
-      s1 = mfma<BF16>(kt[ND + nd], q[nd], s1);
-    }
-    float z[8], top = -INFINITY;
+        for (int t = 0; t < 2 * ND; ++t)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      z[e] = 16 * (e / 4) + 4 * a + e % 4 < live ? (e < 4 ? s0[e] : s1[e - 4]) * P.scale : -INFINITY;
-      top = fmaxf(top, z[e]);
-    }
-    look_up(top);
-    float p[8], r[8];
+          for (int w = 0; w < 4; ++w) top_k = max_pair(top_k, kt[t][w]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m));
-      l += p[e];
-    }
-    // a bf16 operand keeps 8 bits of a probability: the rest goes in as a second one
-    const u32x4 pb = {pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(pb[e / 2] >> (16 * (e & 1))));
-    const u32x4 pr = {pair_as<BF16>(r[0], r[1]), pair_as<BF16>(r[2], r[3]), pair_as<BF16>(r[4], r[5]), pair_as<BF16>(r[6], r[7])};
+          for (int w = 0; w < 4; ++w) top_v = max_pair(top_v, vt[t][w]);
+        top = max_pair(top_k & 0xFFFF, top_k >> 16) | (max_pair(top_v & 0xFFFF, top_v >> 16) << 16);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {                  // rows that are not there have weight 0, but may hold anything
-        const int t0 = 16 * (w / 2) + 4 * a + 2 * (w % 2);
-        vt[t][w] &= (t0 < live ? 0xFFFFu : 0u) | (t0 + 1 < live ? 0xFFFF0000u : 0u);
+        for (int x = 1; x < 64; x <<= 1) top = max_pair(top, (uint32_t)__shfl_xor((int)top, x));
+        if (lane == 0) tops[wave] = top;
       }
-      acc[t] = mfma<BF16>(vt[t], pb, acc[t]);
-      if constexpr (BF16) acc[t] = mfma<BF16>(vt[t], pr, acc[t]);
+      __syncthreads();
+      if (has_tail) {
+        for (int w = 0; w < tails; ++w) top = max_pair(top, tops[w]);
+        const int ek = scale_exponent<BF16>(top & 0xFFFF), ev = scale_exponent<BF16>(top >> 16);
+        const float ik = pow2(-ek), iv = pow2(-ev), cut = t2f<BF16>(cut_bits<BF16>());
+        const float mk = fminf(448.f, cut * ik), mv = fminf(448.f, cut * iv);
+        uint8_t* k_out = P.k_codes + bh * P.cap * D + (int64_t)(codes + wave) * UNIT + lane * 16;
+        uint8_t* v_out = P.v_codes + bh * P.cap * D + (int64_t)(codes + wave) * UNIT + lane * 16;
+#pragma unroll
+        for (int nd = 0; nd < ND; ++nd) {
+          k[nd] = u32x4{codes4<BF16>(kt[nd][0], kt[nd][1], ik, mk), codes4<BF16>(kt[nd][2], kt[nd][3], ik, mk),
+                        codes4<BF16>(kt[ND + nd][0], kt[ND + nd][1], ik, mk), codes4<BF16>(kt[ND + nd][2], kt[ND + nd][3], ik, mk)};
+          v[nd] = u32x4{codes4<BF16>(vt[2 * nd][0], vt[2 * nd][1], iv, mv), codes4<BF16>(vt[2 * nd][2], vt[2 * nd][3], iv, mv),
+                        codes4<BF16>(vt[2 * nd + 1][0], vt[2 * nd + 1][1], iv, mv), codes4<BF16>(vt[2 * nd + 1][2], vt[2 * nd + 1][3], iv, mv)};
+          *reinterpret_cast<u32x4*>(k_out + nd * 1024) = k[nd];
+          *reinterpret_cast<u32x4*>(v_out + nd * 1024) = v[nd];
+        }
+        ck = pow2(ek);
+        cv = pow2(ev);
+        if (wave == 0 && lane == 0) {
+          const int64_t block = bh * (P.cap >> P.log_g) + (codes >> (P.log_g - 5));
+          P.k_scale[block] = ck;
+          P.v_scale[block] = cv;
+        }
+        ready = true;
+      }
+    } else if (has_tail) {
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+      for (int nd = 0; nd < ND; ++nd) {
+        s0 = mfma<BF16>(kt[nd], q[nd], s0);
+        s1 = mfma<BF16>(kt[ND + nd], q[nd], s1);
+      }
+      float z[8], top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        z[e] = 16 * (e / 4) + 4 * a + e % 4 < live ? (e < 4 ? s0[e] : s1[e - 4]) * P.scale : -INFINITY;
+        top = fmaxf(top, z[e]);
+      }
+      look_up(top);
+      float p[8], r[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m));
+        l += p[e];
+      }
+      // a bf16 operand keeps 8 bits of a probability: the rest goes in as a second one
+      const u32x4 pb = {pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(pb[e / 2] >> (16 * (e & 1))));
+      const u32x4 pr = {pair_as<BF16>(r[0], r[1]), pair_as<BF16>(r[2], r[3]), pair_as<BF16>(r[4], r[5]), pair_as<BF16>(r[6], r[7])};
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {                  // rows that are not there have weight 0, but may hold anything
+          const int t0 = 16 * (w / 2) + 4 * a + 2 * (w % 2);
+          vt[t][w] &= (t0 < live ? 0xFFFFu : 0u) | (t0 + 1 < live ? 0xFFFF0000u : 0u);
+        }
+        acc[t] = mfma<BF16>(vt[t], pb, acc[t]);
+        if constexpr (BF16) acc[t] = mfma<BF16>(vt[t], pr, acc[t]);
+      }
     }
   }
 
   // ---- codes; the keys of the next unit are under way while the values of this one are used
-  if (i < stop) {
+  if (!ready && i < stop) {
     load_k();
     load_v();
   }
-  while (i < stop) {
+  while (ready || i < stop) {
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
     for (int nd = 0; nd < ND; ++nd) {
@@ -302,8 +349,11 @@ __global__ void __launch_bounds__(64 * NW, 4) attn8_kernel(const Attn8Params P, 
       s1 = mfma<BF16>(codes_as<BF16>(k[nd][2], k[nd][3]), q[nd], s1);
     }
     const float c = ck * P.scale, f = cv;
-    i += step;
-    step = NW;
+    if (!ready) {
+      i += step;
+      step = NW;
+    }
+    ready = false;
     load_k();
     look_up(fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3]))) * c);
     float p[8];

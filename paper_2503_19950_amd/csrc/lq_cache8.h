@@ -16,7 +16,7 @@ inline int log2_of(int G) { return G == 32 ? 5 : G == 64 ? 6 : 7; }
 
 // What a launch has to know of a batch row.
 struct Row8 {
-  int n;               // tokens that the row holds (append: before the call; a fused step: after it)
+  int n;               // tokens that the row holds (append: before the call; a step: after it)
   int x;               // append: tokens that it takes; attention: its first workgroup
   int parts;           // attention: workgroups that share an item of it (Plan8)
   int b;               // attention: which row
@@ -62,8 +62,9 @@ struct Plan8 {
   int groups, hb;      // head groups of a kv head; heads in each (at most 16, the columns of an operand; the last has the rest)
   int blocks, waves;
 };
-inline int units8(int n, int G) {
-  const int full = n / G * G;
+// (A fused step counts a block that its token fills up among the rows of the tail, which is what it reads.)
+inline int units8(int n, int G, bool step) {
+  const int full = (step ? n - 1 : n) / G * G;
   return full / 32 + 2 * ((n - full + 31) / 32);
 }
 
