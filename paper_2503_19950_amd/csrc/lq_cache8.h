@@ -59,7 +59,7 @@ __device__ __forceinline__ Row8Ptr rows_ptr(const Row8* dev, size_t offset) {
 // tokens, codes as 1 and rows of the tail, twice as wide, as 2.  A workgroup takes an item, or one of `parts` equal parts
 // of it, which the last of them to finish joins.  Rows with the most work come first.
 struct Plan8 {
-  int groups, hb;      // head groups of a kv head; heads in each (at most 16, the columns of an operand; the last has the rest)
+  int groups, hb;      // head groups of a kv head; heads in each (at most 32, two sets of 16; the last has the rest)
   int blocks, waves;
 };
 // (A fused step counts a block that its token fills up among the rows of the tail, which is what it reads.)
@@ -75,12 +75,20 @@ hipError_t launch_read8(const Shape8& s, const lq_cache8& c, int t0, int n, void
 hipError_t launch_attn8(const Shape8& s, const lq_cache8& c, const void* q, float scale, void* out, void* ws, const Plan8& plan,
                         const void* k_new, const void* v_new, const RowArg8& rows, hipStream_t st);
 
-// A workspace: the counters of the items, one to a cache line, then room for the partial results of the workgroups that
-// share an item (they come first in the grid).
+// A workspace: the counters of the items, each item's (one for all its parts, 16 for sixteen of them each) in a cache line,
+// then room for the partial results of the workgroups that share an item (they come first in the grid), and as much again for
+// those of sixteen joined.
 constexpr int CTR8 = 32;           // ints from one counter to the next
 constexpr int MAX_PARTS8 = 1024;
-inline int head_groups8(const Shape8& s) { return (s.gh + 15) / 16; }
-inline size_t counter_bytes8(const Shape8& s) { return (size_t)s.B * s.Hkv * head_groups8(s) * CTR8 * sizeof(int); }
+// Head groups of a kv head.  More than 16 heads are two sets in one workgroup, which read the cache once, or two workgroups,
+// which share the join's work: the former in launches that read 24 MB or more.
+inline int head_groups8(const Shape8& s, bool large) { return (s.gh + (large ? 31 : 15)) / (large ? 32 : 16); }
+inline size_t counter_bytes8(const Shape8& s) { return (size_t)s.B * s.Hkv * head_groups8(s, false) * CTR8 * sizeof(int); }
 inline int partial_floats8(int hb, int d) { return hb * (d + 4); }   // o, then m and l, padded to 16 bytes
+// LDS of a workgroup: each wavefront's results of a set of heads, or a join's (o, m and l of a share for every thread).
+inline int lds_bytes8(int waves, int hb, int d) {
+  const int merge = waves * partial_floats8(hb < 16 ? hb : 16, d), join = waves * 64 * 6;
+  return (merge > join ? merge : join) * (int)sizeof(float);
+}
 
 }  // namespace lq

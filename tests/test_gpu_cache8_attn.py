@@ -23,7 +23,7 @@ def test_lengths_from_none_to_several_blocks(d, G, dtype):
     assert (out[0] == 0).all()
 
 
-@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (2, 1), (3, 1), (5, 1), (16, 1), (17, 1), (24, 1), (33, 1), (40, 2), (12, 4), (64, 8), (32, 32)])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (2, 1), (3, 1), (5, 1), (16, 1), (17, 1), (24, 1), (32, 1), (33, 1), (72, 1), (40, 2), (12, 4), (64, 8), (32, 32)])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_head_layouts(Hq, Hkv, dtype):
     cache, oracle = build(111, 2, Hq, Hkv, 64, 32, dtype, [700, 45])
@@ -32,7 +32,8 @@ def test_head_layouts(Hq, Hkv, dtype):
 
 
 @pytest.mark.parametrize("B,Hq,Hkv,d,G,dtype,L", [
-    (1, 8, 2, 128, 64, "bf16", 20011), (1, 2, 1, 64, 32, "f16", 70001), (3, 8, 1, 96, 128, "bf16", 9001), (1, 4, 4, 128, 32, "f16", 4096),
+    (1, 8, 2, 128, 64, "bf16", 20011), (2, 24, 1, 128, 64, "f16", 12345), (1, 70, 1, 64, 32, "bf16", 9000), (1, 16, 1, 128, 32, "f16", 30001),
+    (1, 5, 1, 96, 64, "bf16", 40000), (1, 2, 1, 64, 32, "f16", 70001), (3, 8, 1, 96, 128, "bf16", 9001), (1, 4, 4, 128, 32, "f16", 4096),
 ])
 def test_long_rows_shared_by_many_workgroups(B, Hq, Hkv, d, G, dtype, L):
     cache, oracle = build(121, B, Hq, Hkv, d, G, dtype, [L] * B)
