@@ -10,8 +10,10 @@
 // A lane of S^T holds four tokens of one head, which are the elements it owes to P^T (tokens permuted inside a unit, as they
 // are stored), and the result of O^T has the heads in the same lanes: nothing but the maximum crosses lanes.
 // Probabilities are 2^(s' - m + 10) with s' = s log2(e) and m the largest s' when it was last looked up, at most 5 behind:
-// they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  The rounding to fp16 (2^-12 of each, unbiased) is
-// left out of the sum of the probabilities, which is kept in fp32.
+// they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  Their rounding to fp16 moves an output by
+// 1.4e-4 of itself, which disappears in the rounding of a bf16 output (1.7e-3), but not in that of an fp16 one (2.1e-4; together
+// 3.0e-4 at 512 tokens): for fp16 caches what the rounding left is a second operand (8 rows of 8192 tokens 27.1 us with and without).  The sum of the probabilities is kept
+// in fp32, before any rounding.
 //
 // Bound by the bytes of the codes.  Workgroups take items or parts of them (Plan8), their wavefronts unit by unit.
 #include <type_traits>
@@ -85,6 +87,19 @@ template <bool BF16>
 __device__ __forceinline__ uint32_t pair_as(float a, float b) {
   if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), half2v));
+}
+
+// eight probabilities as an operand, and what their rounding left as a second one
+template <bool BF16>
+__device__ __forceinline__ u32x4 operand(const float* p) {
+  return u32x4{pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
+}
+template <bool BF16>
+__device__ __forceinline__ u32x4 rest_of(const float* p, u32x4 op) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(op[e / 2] >> (16 * (e & 1))));
+  return operand<BF16>(r);
 }
 
 // over the four lanes of a head (lane % 16)
@@ -338,21 +353,17 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
           top = fmaxf(top, z[e]);
         }
         look_up(x, top);
-        float p[8], r[8];
+        float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m[x]));
           l[x] += p[e];
         }
-        // a bf16 operand keeps 8 bits of a probability: the rest goes in as a second one
-        const u32x4 pb = {pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(pb[e / 2] >> (16 * (e & 1))));
-        const u32x4 pr = {pair_as<BF16>(r[0], r[1]), pair_as<BF16>(r[2], r[3]), pair_as<BF16>(r[4], r[5]), pair_as<BF16>(r[6], r[7])};
+        const u32x4 pb = operand<BF16>(p), pr = rest_of<BF16>(p, pb);     // (a bf16 operand keeps 8 bits, an fp16 one 11)
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           acc[x][t] = mfma<BF16>(vt[t], pb, acc[x][t]);
-          if constexpr (BF16) acc[x][t] = mfma<BF16>(vt[t], pr, acc[x][t]);
+          acc[x][t] = mfma<BF16>(vt[t], pr, acc[x][t]);
         }
       }
     }
@@ -383,7 +394,7 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
     }
     ready = false;
     load_k();
-    u32x4 pb[SETS];
+    u32x4 pb[SETS], pr[SETS];
 #pragma unroll
     for (int x = 0; x < SETS; ++x) {
       const f32x4 y0 = s0[x], y1 = s1[x];
@@ -394,7 +405,8 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
         p[e] = __builtin_amdgcn_exp2f(fmaf(e < 4 ? y0[e] : y1[e - 4], c, BIAS - m[x]));
         l[x] += p[e];
       }
-      pb[x] = u32x4{pair_as<false>(p[0], p[1]), pair_as<false>(p[2], p[3]), pair_as<false>(p[4], p[5]), pair_as<false>(p[6], p[7])};
+      pb[x] = operand<false>(p);
+      if constexpr (!BF16) pr[x] = rest_of<false>(p, pb[x]);
     }
 #pragma unroll
     for (int nd = 0; nd < ND; ++nd) {
@@ -402,7 +414,11 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
       const u32x4 v0 = codes_as<false>(v[nd][0], v[nd][1]), v1 = codes_as<false>(v[nd][2], v[nd][3]);
 #pragma unroll
       for (int x = 0; x < SETS; ++x) {
-        const f32x4 o0 = mfma<false>(v0, pb[x], zero), o1 = mfma<false>(v1, pb[x], zero);
+        f32x4 o0 = mfma<false>(v0, pb[x], zero), o1 = mfma<false>(v1, pb[x], zero);
+        if constexpr (!BF16) {
+          o0 = mfma<false>(v0, pr[x], o0);
+          o1 = mfma<false>(v1, pr[x], o1);
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           acc[x][2 * nd][e] = fmaf(o0[e], f, acc[x][2 * nd][e]);
