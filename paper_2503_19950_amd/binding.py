@@ -576,7 +576,7 @@ class DeviceCache8:
         """Tokens t0 .. t0+n-1 as ([B][Hkv][n][d], [B][Hkv][n][d]) tensors of the cache type: the given ones, whose rows
         behind a sequence are left as they were, or new ones with zeros there."""
         c = self.cfg
-        if n < 1:
+        if n < 1 or t0 < 0 or t0 + n > c.capacity:       # (before room for it is made)
             raise LogQuantError(LQ_ERR_SHAPE, "logquant_read8")
         shape = torch.Size((c.B, c.Hkv, n, c.d))
         k_out, v_out = (torch.zeros(shape, dtype=self.dtype, device=self.device) if t is None else t for t in (k_out, v_out))

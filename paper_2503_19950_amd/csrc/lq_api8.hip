@@ -2,10 +2,10 @@
 #include <math.h>
 #include <stdlib.h>
 
-#include <algorithm>
 
 #include "lq_cache8.h"
 #include "lq_internal.h"
+#include "lq_plan8.h"
 
 using namespace lq;
 
@@ -63,137 +63,10 @@ struct RowList {
   RowArg8 arg(const lq_cache8* c, bool same) const { return RowArg8{e, (Row8*)c->seq_state, n, same}; }
 };
 
-// Parts of an item of u units when none may be larger than `most`.  Up to 20 units, five to a wavefront, it stays whole
-// (512 tokens x 8 kv heads: whole 4.9 us, 2 parts 6.4, 4 parts 6.0; 1024 tokens: 6.9, 7.2, 6.4 and 8 parts 5.8).
-constexpr int WHOLE = 20;
-static int parts_of(int64_t u, int64_t most) { return u > most && u > WHOLE ? (int)((u + most - 1) / most) : 1; }
-
-// The largest load of a compute unit, in units of work, when items over a `whole`-th of it are split into parts of a
-// `shares`-th: the 256 largest workgroups one each, the others from the largest down to the least loaded ones (beyond 512:
-// evenly).
-static int64_t largest_load(const RowList& rows, int per_row, int64_t work, int shares, int whole, const int64_t* units) {
-  constexpr int CUS = 256;
-  struct Class { int64_t size, n; };
-  Class few[ROWS_IN_ARGS];
-  if (rows.n > ROWS_IN_ARGS) return 0;
-  const int64_t most = std::max<int64_t>((work + shares - 1) / shares, 4);
-  for (int b = 0; b < rows.n; ++b) {
-    const int parts = units[b] * whole <= work ? 1 : parts_of(units[b], most);
-    few[b] = Class{(units[b] + parts - 1) / parts, (int64_t)parts * per_row};
-  }
-  std::sort(few, few + rows.n, [](const Class& x, const Class& y) { return x.size > y.size; });
-  int64_t load = few[0].size, left = CUS;
-  int i = 0;                                           // the class that the 256 largest end in
-  while (i < rows.n && few[i].n < left) left -= few[i++].n;
-  if (i == rows.n) return load;
-  int up = i, down = i;
-  int64_t room = left, more = few[i].n - left;         // of class `up` among the 256; of class `down` behind them
-  for (int64_t paired = 0; paired < CUS;) {
-    while (more == 0 && ++down < rows.n) more = few[down].n;
-    while (room == 0 && --up >= 0) room = few[up].n;
-    if (down >= rows.n || up < 0) break;
-    const int64_t n = std::min(room, more);
-    load = std::max(load, few[up].size + few[down].size);
-    room -= n;
-    more -= n;
-    paired += n;
-  }
-  int64_t rest = down < rows.n ? more * few[down].size : 0;
-  for (int k = down + 1; k < rows.n; ++k) rest += few[k].n * few[k].size;
-  return load + rest / CUS;
-}
-
-// Fills the rows' parts, order and first workgroups, and says whether the rows still are alike.
-//
-// A compute unit reads up to 1.5 times its share of the memory's rate, so a launch is as fast as the memory where no compute
-// unit has much more than a 256th of the work, and 256 workgroups, of 4 wavefronts already, are placed one to a compute unit.
-// Times in us, d = 128, 4 heads a kv head, before (items whole, or in parts of a 256th rounded up) and with each rule:
-//  - items that are fewer: as many parts each as make up to 256 workgroups (24 items of 16384 tokens: 11 parts, 264
-//    workgroups, 25.7; 10 parts 20.6), none of less than 4 units, one to a wavefront.
-//  - between 128 and 256 items that cannot be split evenly stay whole, up to 200 of them in workgroups of 8 wavefronts, which
-//    use that reserve (132 items of 4096 tokens: 4 wavefronts 31.3, 8 27.7; 180 items 34.3 and 34.6); so do long parts of
-//    d = 64, whose units are half as large (5 rows of 34665 x 8 kv heads 36.9 -> 34.8, 4 of 20000 x 4: 10.8 and 12.0).
-//  - a few items more than 256: rows for 256 stay whole, the rest is split into 256 (260 items 59.5 -> 50.9; 304 items
-//    64.4 -> 56.9; from 340 on the reserve covers the second item of a compute unit).
-// Rows of different lengths:
-//  - up to 256 items: the smallest `most` that makes no more than 256 parts (16 rows of up to 8000 x 8 kv heads 36.1 -> 31.9;
-//    4 rows of up to 30000 34.8 -> 28.7), if that is within 1.5 of the even share.
-//  - else what is over a 200th of all work is split into parts of a 256th, or, of up to 256 items, over a 300th into parts of
-//    a 384th where that loads the compute units more evenly (45 rows of up to 24597 x 4 kv heads 132 -> 108, but 1 of 65536
-//    and 29 of 512 x 8: 33.6 and 40.0).  Few and large workgroups, of 8 or 16 wavefronts, the longest first, leave the balance
-//    to their placement (64 rows of up to 4096 x 8 kv heads: 4 wavefronts 54.5, 8 54.6, 16 49.5; 100 of up to 4000: 79.9, 75.8,
-//    76.4; 30 of up to 9000, d = 96: 43.0, 43.6, 47.0), unless they are small (200 rows of up to 2000, 31 units each: 4
-//    wavefronts 75.6, 16 84.6) or many, which balance by their number.
-static bool plan8(const Shape8& s, bool same, bool step, RowList* rows, Plan8* p) {
-  constexpr int CUS = 256, LEAST = 4;
-  auto units = [&](const Row8& r) -> int64_t { return units8(r.n, s.G, step); };
-  int64_t tokens = 0;
-  for (int b = 0; b < rows->n; ++b) tokens += rows->e[b].n;
-  p->groups = head_groups8(s, tokens * s.Hkv * s.d * 2 >= 24000000);
-  p->hb = (s.gh + p->groups - 1) / p->groups;
-  p->waves = 4;
-  const int per_row = s.Hkv * p->groups;
-  const int64_t items = (int64_t)s.B * per_row;
-  Row8 *first = rows->e, *last = rows->e + rows->n;
-  if (same) {
-    const int u = (int)units(*first), most_parts = u > WHOLE ? u / LEAST : 1;
-    const int parts = items <= CUS / 2 ? std::min((int)(CUS / items), most_parts) : 1;
-    for (Row8* r = first; r != last; ++r) r->parts = parts;
-    if ((items > CUS / 2 && items <= 200) || (s.d == 64 && items <= CUS / 2 && u >= 100 * parts)) p->waves = 8;
-    if (items > CUS && items < 340 && per_row <= CUS) {
-      const int left = s.B - CUS / per_row;
-      const int split = std::min(CUS / (left * per_row), most_parts);
-      if (split > 1) {
-        for (Row8* r = first; r != first + left; ++r) r->parts = split;
-        same = false;
-      }
-    }
-  } else {
-    int64_t work = 0, longest = LEAST, most = 0;
-    for (Row8* r = first; r != last; ++r) {
-      const int64_t u = units(*r);
-      work += u * per_row;
-      longest = std::max(longest, u);
-    }
-    if (items <= CUS) {
-      int64_t lo = LEAST, hi = longest;
-      while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        int64_t n = 0;
-        for (Row8* r = first; r != last; ++r) n += parts_of(units(*r), mid);
-        if (n * per_row <= CUS) hi = mid; else lo = mid + 1;
-      }
-      if (lo == LEAST || 2 * lo * CUS <= 3 * work) most = lo;
-    }
-    if (most) {
-      for (Row8* r = first; r != last; ++r) r->parts = parts_of(units(*r), most);
-    } else {
-      int shares = CUS, whole = 200;
-      if (items <= CUS && rows->n <= ROWS_IN_ARGS) {
-        int64_t u[ROWS_IN_ARGS];
-        for (int b = 0; b < rows->n; ++b) u[b] = units(rows->e[b]);
-        if (largest_load(*rows, per_row, work, 384, 300, u) < largest_load(*rows, per_row, work, CUS, 200, u)) shares = 384, whole = 300;
-      }
-      most = std::max<int64_t>((work + shares - 1) / shares, LEAST);
-      for (Row8* r = first; r != last; ++r) r->parts = units(*r) * whole <= work ? 1 : parts_of(units(*r), most);
-      if (items <= 1024 && work >= 24 * items) p->waves = items <= CUS ? 8 : 16;
-    }
-    // (by work, not by tokens: what is split has to come first)
-    std::sort(first, last, [&](const Row8& x, const Row8& y) { return units(x) > units(y); });
-  }
-  while (lds_bytes8(p->waves, p->hb, s.d) > 65536 || (p->hb > 16 && p->waves > 4)) p->waves /= 2;   // (LDS that a launch may ask for)
-  p->blocks = 0;
-  for (Row8* r = first; r != last; ++r) {
-    r->x = p->blocks;
-    p->blocks += r->parts * per_row;
-  }
-  return same;
-}
-
 static lq_status attend8(const Shape8& s, const lq_cache8& c, RowList* rows, const void* k_new, const void* v_new, const void* q,
                          float softmax_scale, void* out, void* workspace, hipStream_t stream) {
   Plan8 plan;
-  const bool same = plan8(s, rows->alike(), k_new != nullptr, rows, &plan);
+  const bool same = plan8(s, rows->alike(), k_new != nullptr, rows->e, rows->n, &plan);
   if (!(softmax_scale > 0.f)) softmax_scale = 1.0f / sqrtf((float)s.d);
   return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, rows->arg(&c, same), stream) == hipSuccess ? LQ_OK
                                                                                                                              : LQ_ERR_HIP;

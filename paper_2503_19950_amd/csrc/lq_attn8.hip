@@ -159,18 +159,12 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
   }
   // Workgroups i and i + 8 are on the same die, with an L2 of its own: the head groups of a kv head, which read the same codes
   // in the same order, are that far apart.
-  int pair = local, g = 0;                             // (kv head, part), head group
-  if (P.groups > 1) {
-    const int begin = local / (8 * P.groups) * 8, in = local - begin * P.groups;
-    const int wide = P.Hkv * parts - begin < 8 ? P.Hkv * parts - begin : 8;
-    g = in / wide;
-    pair = begin + in - g * wide;
-  }
+  const Pair8 of = pair8(local, P.groups, P.Hkv * parts);
+  const int pair = of.pair, g = of.g;                  // (kv head, part), head group
   const int h = pair / parts, part = pair - h * parts, j = h * P.groups + g;
   const int first_slot = (int)blockIdx.x - local + j * parts;               // of the item's partial results
-  const int codes = (STEP ? n - 1 : n) >> P.log_g << (P.log_g - 5), rest = n - 32 * codes;   // units of codes, rows of the tail
-  const int work = codes + 2 * ((rest + 31) / 32), size = (work + parts - 1) / parts;
-  const int pos = part * size, to = pos + size < work ? pos + size : work;
+  const Part8 mine = part8(n, part, parts, P.log_g, STEP);
+  const int codes = mine.codes, rest = mine.rest, pos = mine.pos, stop = mine.stop, tails = mine.tails;
   const int64_t bh = (int64_t)b * P.Hkv + h;
   const int heads = P.hb < P.gh - g * P.hb ? P.hb : P.gh - g * P.hb;
   const int64_t head0 = bh * P.gh + g * P.hb;
@@ -184,14 +178,10 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
       for (int nd = 0; nd < ND; ++nd) q[x][nd] = load16(rs, (16 * x + head) * D * 2 + a * 16 + nd * 64);
   }
 
-  // The tail belongs to the last part.  Its units go to the first wavefronts, one each, which sit out two rounds of codes for
-  // it: they are the oldest, and their loads are served first.
-  const int tails = part == parts - 1 ? (rest + 31) / 32 : 0;
+  // (The first wavefronts, which have the tail, are the oldest, and their loads are served first.)
   const bool has_tail = wave < tails;
-  const int workers = tails < NW ? NW - tails : NW;                       // wavefronts in the first two rounds
-  const int stop = to < codes ? to : codes;
-  const bool sits_out = has_tail && workers < NW;
-  int i = pos + (sits_out ? wave + 2 * workers : wave - (NW - workers)), step = sits_out ? NW : workers;
+  const Deal8 deal = deal8(mine, wave, NW);
+  int i = deal.first, step = deal.step;
 
   const __amdgpu_buffer_rsrc_t rk = buffer(P.k_codes + bh * P.cap * D, stop * UNIT);   // behind the last unit: zeros, no reads
   const __amdgpu_buffer_rsrc_t rv = buffer(P.v_codes + bh * P.cap * D, stop * UNIT);
@@ -206,10 +196,9 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
   const int turn = len > 0 ? (int)((uint64_t)((uint32_t)((int)blockIdx.x - local + pair) * 0x9E3779B1u) * (uint32_t)len >> 32) : 0;
   u32x4 k[ND], v[ND];
   float ck, cv;
-  int unit;                                            // the i-th of the part, counted from there; behind the last: `stop`
+  int unit;                                            // the i-th, counted from there
   auto load_k = [&]() {
-    unit = i + turn < stop ? i + turn : i + turn - len;
-    if (i >= stop) unit = stop;
+    unit = turned8(mine, i, turn);
 #pragma unroll
     for (int nd = 0; nd < ND; ++nd) k[nd] = load16(rk, unit * UNIT + lane * 16 + nd * 1024);
     const int block = i < stop ? unit >> (P.log_g - 5) : 0;

@@ -101,6 +101,21 @@ def test_many_heads_in_large_workgroups(dtype, gh, lengths):
     U.check_output(cache.decode_attn(q.to(U.DEVICE)), q, oracle, dtype, rows_of=[0, 1, B // 2, B - 1])
 
 
+@pytest.mark.parametrize("B,gh,d,G,dtype,L", [(4, 24, 64, 32, "f16", 48030), (1, 32, 128, 64, "bf16", 95038), (2, 17, 96, 128, "f16", 65150),
+                                              (3, 40, 64, 128, "bf16", 64126)])
+def test_more_than_16_heads_over_a_long_context(B, gh, d, G, dtype, L):
+    """Two sets of heads in a workgroup (from 24 MB on), attention and steps across the end of a block."""
+    cache, oracle = build(361, B, gh, 1, d, G, dtype, [L] + [L - 1001 * b for b in range(1, B)], capacity=(L // G + 2) * G)
+    q = queries(362, B, gh, d, dtype)
+    U.check_output(cache.decode_attn(q.to(U.DEVICE)), q, oracle, dtype)
+    for i in range(3):
+        k, v, q = U.rows(370 + i, B, 1, 1, d, dtype), U.rows(380 + i, B, 1, 1, d, dtype), queries(390 + i, B, gh, d, dtype)
+        out = cache.decode_step(k.to(U.DEVICE), v.to(U.DEVICE), q.to(U.DEVICE))
+        oracle.append(k, v)
+        U.check_output(out, q, oracle, dtype)
+    oracle.check(cache)
+
+
 def test_counts_set_back_within_a_block():
     """Tokens that are dropped again: within the tail, and from a block that single tokens have just filled."""
     G, d = 64, 64

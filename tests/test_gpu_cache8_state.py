@@ -160,4 +160,12 @@ def test_tensors_of_another_kind_are_refused():
             cache.decode_step(one, one, y)
     with pytest.raises(ValueError):
         cache.append(x, x, [1])
+    from paper_2503_19950_amd.binding import LogQuantError
+    for t0, n in ((0, 0), (-1, 2), (0, cache.cfg.capacity + 1), (cache.cfg.capacity, 1), (0, 2 ** 40)):
+        with pytest.raises(LogQuantError):
+            cache.read(t0, n)
+    with pytest.raises(LogQuantError):
+        cache.append(x, x, [5, 0])
+    with pytest.raises(LogQuantError):
+        cache.append(x, x, [-1, 0])
     assert cache.counts() == [40, 3]
