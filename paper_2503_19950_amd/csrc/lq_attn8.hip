@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
 
   // ---- the workgroups of an item together: the last one to come joins them, nobody waits.  Many are joined by sixteens first
   // (2 kv heads of 43162 tokens in 128 parts: 19.0 -> 11.8 us).
-  constexpr int T = 64 * NW, BATCH = 8, FAN = 16;
+  constexpr int T = 64 * NW, BATCH = 8, FAN = FAN8;
   __shared__ int last;
   const int cols = heads * (D / 4), shares = cols < T ? T / cols : 1;
   int* ctr = P.counters + (int64_t)(b * per_row + j) * CTR8;

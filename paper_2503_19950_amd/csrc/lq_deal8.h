@@ -80,9 +80,10 @@ LQ8_HD int turned8(const Part8& p, int i, int turn) {
   return i + turn < p.stop ? i + turn : i + turn - (p.stop - p.pos);
 }
 
-// A workspace: the counters of the items, each item's (one for all its parts, 16 for sixteen of them each) in a cache line,
+// A workspace: the counters of the items, each item's (one for all its parts, others for sixteen of them each) in a cache line,
 // then room for the partial results of the workgroups that share an item (they come first in the grid), and as much again for
 // those of sixteen joined.
+constexpr int FAN8 = 16;           // parts joined at a time where there are many
 constexpr int CTR8 = 32;           // ints from one counter to the next
 constexpr int MAX_PARTS8 = 1024;
 // Head groups of a kv head.  More than 16 heads are two sets in one workgroup, which read the cache once, or two workgroups,

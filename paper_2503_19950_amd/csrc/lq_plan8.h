@@ -51,7 +51,9 @@ inline int64_t largest_load(int rows, const int64_t* units, int per_row, int64_t
 // unit has much more than a 256th of the work, and 256 workgroups, of 4 wavefronts already, are placed one to a compute unit.
 // Times in us, d = 128, 4 heads a kv head, before (items whole, or in parts of a 256th rounded up) and with each rule:
 //  - items that are fewer: as many parts each as make up to 256 workgroups (24 items of 16384 tokens: 11 parts, 264
-//    workgroups, 25.7; 10 parts 20.6), none of less than 4 units, one to a wavefront.
+//    workgroups, 25.7; 10 parts 20.6), none of less than 4 units, one to a wavefront; a single item in up to 128 (160000
+//    tokens: 128 parts 13.0, 256 15.2), and no more than are joined in one go where 20 units each are enough for that (8 heads,
+//    4000 tokens: 16 parts 7.0, 31 8.5; 16 heads, 10000: 11.0 and 12.7).
 //  - between 128 and 256 items that cannot be split evenly stay whole, up to 200 of them in workgroups of 8 wavefronts, which
 //    use that reserve (132 items of 4096 tokens: 4 wavefronts 31.3, 8 27.7; 180 items 34.3 and 34.6); so do long parts of
 //    d = 64, whose units are half as large (5 rows of 34665 x 8 kv heads 36.9 -> 34.8, 4 of 20000 x 4: 10.8 and 12.0).
@@ -79,12 +81,14 @@ inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows,
   Row8 *first = rows, *last = rows + n_rows;
   if (same) {
     const int u = (int)units(*first), most_parts = u > WHOLE8 ? u / LEAST : 1;
-    const int parts = items <= CUS / 2 ? std::min((int)(CUS / items), most_parts) : 1;
+    int parts = items <= CUS / 2 ? std::min({(int)(CUS / items), CUS / 2, most_parts}) : 1;
+    const int at_once = FAN8 * std::max(64 * p->waves / (p->hb * s.d / 4), 1);          // parts that are joined in one go
+    if (parts > at_once && u <= 20 * at_once) parts = at_once;
     for (Row8* r = first; r != last; ++r) r->parts = parts;
     if ((items > CUS / 2 && items <= 200) || (s.d == 64 && items <= CUS / 2 && u >= 100 * parts)) p->waves = 8;
     if (items > CUS && items < 340 && per_row <= CUS) {
       const int left = s.B - CUS / per_row;
-      const int split = std::min(CUS / (left * per_row), most_parts);
+      const int split = std::min({CUS / (left * per_row), CUS / 2, most_parts});
       if (split > 1) {
         for (Row8* r = first; r != first + left; ++r) r->parts = split;
         same = false;

@@ -98,7 +98,7 @@ int main() {
           if (len > 0) CHECK(rounds <= len / p.waves + 3);
         }
       }
-      CHECK(r.parts <= 16 * (CTR8 - 1));                              // counters for sixteen parts each
+      CHECK(r.parts <= FAN8 * (CTR8 - 1));                              // counters for sixteen parts each
       if (!first_of_kind) continue;
       const Part8 all = part8(r.n, 0, 1, log_g, step);
       for (int j = 0; j < per_row; ++j) {
