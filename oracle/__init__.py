@@ -19,11 +19,13 @@ attention  : Eq. 2 with the 1/sqrt(d) of Eq. 6 over [fp rows || dequantized rows
 diagnostics: L1 distance between the exact attention distribution and the one seen
              after quantizing or evicting the tokens a selection rule does not keep
              (synthetic analogue of Table 2, Sec. 2.3).
+cache8     : the 8-bit cache of one slice: blocks of tokens as e4m3 codes with one
+             power-of-two scale, the newest tokens at original precision, and its layout.
 layout     : the physical index functions documented in include/logquant.h,
              re-implemented independently so packed words can be compared
              bit for bit.
 
-Parity status: selection, quantizer, attention, diagnostics and layout are pinned by
+Parity status: selection, quantizer, attention, diagnostics, cache8 and layout are pinned by
 tests/test_oracle_*.py against hand traces of Algorithm 1, closed forms,
 brute force, exact rational arithmetic, textbook softmax attention and
 permutation invariance.  Accuracy-level behaviour (the paper's Tables 1-4,

@@ -12,10 +12,17 @@
 // Probabilities are 2^(s' - m + 10) with s' = s log2(e) and m the largest s' when it was last looked up, at most 5 behind:
 // they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  Their rounding to fp16 moves an output by
 // 1.4e-4 of itself, which disappears in the rounding of a bf16 output (1.7e-3), but not in that of an fp16 one (2.1e-4; together
-// 3.0e-4 at 512 tokens): for fp16 caches what the rounding left is a second operand (8 rows of 8192 tokens 27.1 us with and without).  The sum of the probabilities is kept
-// in fp32, before any rounding.
+// 3.0e-4 at 512 tokens): for fp16 caches what the rounding left is a second operand (8 rows of 8192 tokens 27.1 us with and
+// without).  The sum of the probabilities is kept in fp32, before any rounding.
 //
-// Bound by the bytes of the codes.  Workgroups take items or parts of them (Plan8), their wavefronts unit by unit.
+// Bound by the bytes of the codes.  A unit of d = 128 (8 KB) costs a wavefront about 200 vector and 16 to 24 matrix
+// instructions, a quarter of what a compute unit has time for while its share of them arrives.  Keys of the next unit are
+// loaded while the values of this one are used, in the same registers, so that 4 wavefronts fit a SIMD; one to three units
+// more in flight brought nothing.  131072 tokens x 8 kv heads, bf16, 269 MB: 48.9 us, 5.5 TB/s; of these 1.7 us until the first
+// keys are there, 40.5 in the loop (6.6 TB/s), 3 between the first and the last wavefront to end, 3 to join 32 parts.
+// 16 rows x 32 heads x 32768, d = 96, 3.2 GB: 520 us, 6.2 TB/s, 0.97 of what a plain read reaches.
+//
+// Workgroups take items or parts of them (lq_plan8.h), their wavefronts unit by unit (lq_deal8.h).
 #include <type_traits>
 
 #include "lq_cache8.h"
