@@ -403,6 +403,8 @@ lq_status logquant_read8(const lq_config8 *cfg, const lq_cache8 *cache, int32_t 
 /* Decode attention over the 8-bit cache: out[b][h] = softmax_t(scale * q[b][h] . k_t)
  * applied to v_t, t running over the tokens that row b holds, with the values that
  * logquant_read8 gives (codes and scales are applied in registers); zeros for an empty row.
+ * Elements of q and v are assumed to stay below 2^90 and logits within fp32 (always true of
+ * fp16; bf16 sums over larger ones would overflow).
  *   q, out, softmax_scale, workspace: as for logquant_decode_attn (sizes from
  *   logquant_sizes8, prepared with logquant_workspace_init8). */
 lq_status logquant_decode_attn8(const lq_config8 *cfg, const lq_cache8 *cache, const void *q,

@@ -159,6 +159,19 @@ def test_logits_that_rise_and_fall_along_a_row(dtype):
         U.check_output(cache.decode_attn(q.to(U.DEVICE)), q, oracle, dtype)
 
 
+@pytest.mark.parametrize("q_gain,k_gain,v_gain", [(2.0 ** 40, 2.0 ** -40, 2.0 ** 85), (2.0 ** -60, 2.0 ** 60, 2.0 ** -100), (2.0 ** 80, 2.0 ** -80, 2.0 ** -120)])
+def test_far_magnitudes_of_bf16(q_gain, k_gain, v_gain):
+    """Scales of blocks near the ends of their range: the outputs are those of ordinary magnitudes, times v's."""
+    cache = U.make(2, 4, 2, 96, 32, "bf16", 1024)
+    oracle = U.Oracle(cache, "bf16")
+    K, V = U.rows(157, 2, 2, 1000, 96, "bf16", k_gain), U.rows(158, 2, 2, 1000, 96, "bf16", v_gain, outliers=False)
+    oracle.append(K, V)
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE))
+    oracle.check(cache)
+    q = queries(159, 2, 4, 96, "bf16", q_gain)
+    U.check_output(cache.decode_attn(q.to(U.DEVICE)), q, oracle, "bf16")
+
+
 def test_a_sink_ahead_of_a_long_even_context():
     """One heavy token sets the reference, tens of thousands 2^16 below it weigh as much as it does."""
     d, L = 64, 60000
