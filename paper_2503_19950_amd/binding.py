@@ -527,14 +527,15 @@ class DeviceCache8:
         self.c = lq_cache8(*[getattr(self, name).data_ptr() for name in self.BUFFERS], C.cast(self.n, _I32P),
                            self.seq_state.data_ptr())
         # what every call takes, made once (a decode call's host time 6.5 -> 5.1 us)
+        self._index = self.device.index
         self._cfg, self._c, self._ws = C.byref(cfg), C.byref(self.c), self.workspace.data_ptr()
         self._q_shape, self._token = torch.Size((cfg.B, cfg.Hq, cfg.d)), torch.Size((cfg.B, cfg.Hkv, 1, cfg.d))
         self._call("logquant_workspace_init8", self._ws)
 
     def _call(self, name, *args):
-        i = self.device.index
+        i = self._index
         f = getattr(_lib, name)
-        if torch.cuda.current_device() == i:
+        if torch._C._cuda_getDevice() == i:
             st = f(self._cfg, *args, torch._C._cuda_getCurrentRawStream(i))
         else:
             with torch.cuda.device(i):
@@ -543,7 +544,7 @@ class DeviceCache8:
             raise LogQuantError(st, name)
 
     def _address(self, name, t, shape):
-        if t.shape != shape or t.dtype != self.dtype or t.device != self.device or not t.is_contiguous():
+        if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError("%s: expected a contiguous %s tensor of shape %s on %s" % (name, self.dtype, tuple(shape), self.device))
         return t.data_ptr()
 

@@ -36,7 +36,7 @@ struct Plan8 {
 };
 // (A fused step counts a block that its token fills up among the rows of the tail, which is what it reads.)
 inline int units8(int n, int G, bool step) {
-  const int full = (step ? n - 1 : n) / G * G;
+  const int full = (step ? n - 1 : n) & -G;            // (G is a power of two)
   return full / 32 + 2 * ((n - full + 31) / 32);
 }
 

@@ -70,9 +70,11 @@ inline int64_t largest_load(int rows, const int64_t* units, int per_row, int64_t
 //    wavefronts 75.6, 16 84.6) or many, which balance by their number.
 inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows, Plan8* p) {
   constexpr int CUS = 256, LEAST = 4;
-  auto units = [&](const Row8& r) -> int64_t { return units8(r.n, s.G, step); };
   int64_t tokens = 0;
-  for (int b = 0; b < n_rows; ++b) tokens += rows[b].n;
+  for (int b = 0; b < n_rows; ++b) {
+    tokens += rows[b].n;
+    rows[b].x = units8(rows[b].n, s.G, step);          // until the end
+  }
   p->groups = head_groups8(s, tokens * s.Hkv * s.d * 2 >= 24000000);
   p->hb = (s.gh + p->groups - 1) / p->groups;
   p->waves = 4;
@@ -80,7 +82,7 @@ inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows,
   const int64_t items = (int64_t)s.B * per_row;
   Row8 *first = rows, *last = rows + n_rows;
   if (same) {
-    const int u = (int)units(*first), most_parts = u > WHOLE8 ? u / LEAST : 1;
+    const int u = first->x, most_parts = u > WHOLE8 ? u / LEAST : 1;
     int parts = items <= CUS / 2 ? std::min({(int)(CUS / items), CUS / 2, most_parts}) : 1;
     const int at_once = FAN8 * std::max(64 * p->waves / (p->hb * s.d / 4), 1);          // parts that are joined in one go
     if (parts > at_once && u <= 20 * at_once) parts = at_once;
@@ -97,7 +99,7 @@ inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows,
   } else {
     int64_t work = 0, longest = LEAST, most = 0;
     for (Row8* r = first; r != last; ++r) {
-      const int64_t u = units(*r);
+      const int64_t u = r->x;
       work += u * per_row;
       longest = std::max(longest, u);
     }
@@ -106,26 +108,26 @@ inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows,
       while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;
         int64_t n = 0;
-        for (Row8* r = first; r != last; ++r) n += parts_of(units(*r), mid);
+        for (Row8* r = first; r != last; ++r) n += parts_of(r->x, mid);
         if (n * per_row <= CUS) hi = mid; else lo = mid + 1;
       }
       if (lo == LEAST || 2 * lo * CUS <= 3 * work) most = lo;
     }
     if (most) {
-      for (Row8* r = first; r != last; ++r) r->parts = parts_of(units(*r), most);
+      for (Row8* r = first; r != last; ++r) r->parts = parts_of(r->x, most);
     } else {
       int shares = CUS, whole = 200;
       if (items <= CUS && n_rows <= ROWS_IN_ARGS) {
         int64_t u[ROWS_IN_ARGS];
-        for (int b = 0; b < n_rows; ++b) u[b] = units(rows[b]);
+        for (int b = 0; b < n_rows; ++b) u[b] = rows[b].x;
         if (largest_load(n_rows, u, per_row, work, 384, 300) < largest_load(n_rows, u, per_row, work, CUS, 200)) shares = 384, whole = 300;
       }
       most = std::max<int64_t>((work + shares - 1) / shares, LEAST);
-      for (Row8* r = first; r != last; ++r) r->parts = units(*r) * whole <= work ? 1 : parts_of(units(*r), most);
+      for (Row8* r = first; r != last; ++r) r->parts = (int64_t)r->x * whole <= work ? 1 : parts_of(r->x, most);
       if (items <= 1024 && work >= 24 * items) p->waves = items <= CUS ? 8 : 16;
     }
     // (by work, not by tokens: what is split has to come first)
-    std::sort(first, last, [&](const Row8& x, const Row8& y) { return units(x) > units(y); });
+    std::sort(first, last, [](const Row8& x, const Row8& y) { return x.x > y.x; });
   }
   while (lds_bytes8(p->waves, p->hb, s.d) > 65536 || (p->hb > 16 && p->waves > 4)) p->waves /= 2;   // (LDS that a launch may ask for)
   p->blocks = 0;
