@@ -6,10 +6,9 @@
 // channels c and c + 16; it loads two neighbouring channels of eight tokens (4 bytes each, 64 in a row per 16 lanes) and
 // trades half of the packed codes with the lane eight places away.
 //
-// 131072 tokens x 8 kv heads, bf16 (805 MB): written in 144 us (5.6 TB/s, two thirds of it reads), read back in 150 us (5.4, two
-// thirds of it writes); a copy of 1 GB moves 5.05 TB/s.  Eight rows of up to 8191, G = 32 (203 MB): 47.7 us, 4.3 TB/s, the start
-// and end of 8000 short workgroups.  Wavefronts with a block of 32 tokens each to themselves took 52.5, rows staged through LDS
-// 45.5 but 146 for the long prompt.
+// 131072 tokens x 8 kv heads, bf16 (805 MB): written in 143 us (5.6 TB/s, two thirds of it reads), read back in 150 us (5.4, two
+// thirds of it writes); a copy of 1 GB moves 5.05 TB/s.  Eight rows of up to 8191, G = 32 (203 MB): 40.3 us, 5.0 TB/s.  Wavefronts
+// with a block of 32 tokens each to themselves, or values staged through LDS, were no faster.
 #include "lq_cache8.h"
 #include "lq_device.h"
 #include "lq_internal.h"
@@ -67,20 +66,37 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {   // reads beyond it: zeros
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0); }
+__device__ __forceinline__ uint4 load16(__amdgpu_buffer_rsrc_t rs, int off) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
 // token within its unit of 32 at position e of the eight that lane row a holds: 16 b + 4 a + e % 4, b = e / 4
 __device__ __forceinline__ int value_token(int a, int e) { return 16 * (e >> 2) + 4 * a + (e & 3); }
 
 // grid (most blocks that a row completes, plus one, B * Hkv).  Workgroup i of a slice quantizes the i-th block that becomes
 // full; the rows left over go to the tail by workgroup `blocks completed`, or by workgroup 0 where its block takes rows
-// from the tail, after it has read them.
+// from the tail, after it has read them.  These come first in the grid, slice by slice, and the others behind them: in its
+// place among a slice's workgroups the last of them, which has up to twice the others' work, was the launch's end (8 rows of
+// 8192 tokens x 8 kv heads behind 127 rows of the tail 101 -> 77.5 us, of which 75 without the tail; rows of up to 8191, G = 32,
+// 43.9 -> 40.3).
 template <bool BF16, int D, int G, int MODE>
 __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params P, const Rows8<MODE> S) {
   (void)S;
   constexpr int ND = D / 32, PIECES = G / 32 * ND, MINE = (PIECES + WAVES - 1) / WAVES;
-  const int bh = blockIdx.y, i = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int slices = gridDim.y, blocks = gridDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int at_grid = blockIdx.y * blocks + blockIdx.x, behind = at_grid - slices;
+  const int bh = behind < 0 ? at_grid : behind / (blocks - 1);
   const Row8 row = row_of<Append8Params, MODE>(P, bh / P.Hkv);
   const int held = row.n % G, all = held + row.x, full = all / G;   // rows from the first open block on; blocks completed
   const int tail_wg = held && full ? 0 : full;
+  const int early = tail_wg < blocks ? tail_wg : blocks - 1, other = behind - bh * (blocks - 1);
+  const int i = behind < 0 ? early : other < early ? other : other + 1;
   if (i > full || (i == full && i != tail_wg) || row.x == 0) return;
   const uint16_t* k_new = P.k_new + (int64_t)bh * P.n_max * D;
   const uint16_t* v_new = P.v_new + (int64_t)bh * P.n_max * D;
@@ -91,6 +107,7 @@ __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params
     const int64_t block = row.n / G + i;
     const bool from_tail = i == 0 && held;
     const int first = i * G - held;                  // of the block's rows among the new ones
+    const __amdgpu_buffer_rsrc_t new_v = buffer(v_new, (G - held) * (2 * D));   // those that block 0 takes; elsewhere: zeros, not read
     uint4 k[MINE][2];
     uint32_t v[MINE][8];
     uint32_t top_k = 0, top_v = 0;
@@ -106,13 +123,21 @@ __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params
         k[j][h] = *reinterpret_cast<const uint4*>(src);
       }
       const int c = 32 * nd + 2 * (lane % 16);
+      if (!from_tail) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = 32 * unit + value_token(lane / 16, e);
-        if (from_tail && t < held)
-          v[j][e] = (uint32_t)v_tail[v_fp_index(t, c, 2 * ND)] | ((uint32_t)v_tail[v_fp_index(t, c + 1, 2 * ND)] << 16);
-        else
-          v[j][e] = *reinterpret_cast<const uint32_t*>(v_new + (int64_t)(first + t) * D + c);
+        for (int e = 0; e < 8; ++e)
+          v[j][e] = *reinterpret_cast<const uint32_t*>(v_new + (int64_t)(first + 32 * unit + value_token(lane / 16, e)) * D + c);
+      } else {                                       // two pieces of the tail as they lie, eight tokens of c and of c + 1, and the new ones
+        const uint4* old = reinterpret_cast<const uint4*>(v_tail + v_fp_index(32 * unit + 4 * (lane / 16), c, 2 * ND));
+        const uint4 x = old[0], y = old[1];
+        const uint32_t lo[4] = {x.x, x.y, x.z, x.w}, hi[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = 32 * unit + value_token(lane / 16, e);
+          const uint32_t was = __builtin_amdgcn_perm(hi[e / 2], lo[e / 2], e & 1 ? 0x07060302 : 0x05040100);
+          const uint32_t is = load4(new_v, (t - held) * (2 * D) + 2 * c);
+          v[j][e] = t < held ? was : is;
+        }
       }
     }
 #pragma unroll
@@ -173,14 +198,52 @@ __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params
   // tail has just become full and nothing follows, its new rows, so that the count can be set back into it
   const bool keep = held && all == G;
   const int at = full && !keep ? 0 : held, left = (keep ? G : all - full * G) - at, from = keep ? 0 : full * G + at - held;
-  for (int x = threadIdx.x; x < left * (D / 8); x += 64 * WAVES) {
-    const int j = x / (D / 8), c = x % (D / 8) * 8;
-    const int64_t src = (int64_t)(from + j) * D + c;
-    *reinterpret_cast<uint4*>(k_tail + k_fp_index(at + j, c, ND)) = *reinterpret_cast<const uint4*>(k_new + src);
-    const uint4 y = *reinterpret_cast<const uint4*>(v_new + src);
-    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+  // In pieces of the tail as it lies: 16 rows next to each other for keys; for values two channels of eight rows, of which
+  // those that are all new are stored at once, and all loads first (64 slices with 63 rows left over behind 127 blocks: row by
+  // row, values 2 bytes at a time, 105 us; so 80).
+  const int end = at + left;
+  const __amdgpu_buffer_rsrc_t src_k = buffer(k_new + (int64_t)from * D, left * (2 * D)), src_v = buffer(v_new + (int64_t)from * D, left * (2 * D));
+  constexpr int T = 64 * WAVES, NK = (G * D / 8 + T - 1) / T, NV = (G * D / 16 + T - 1) / T;
+  uint4 k[NK];
+  uint32_t v[NV][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v_tail[v_fp_index(at + j, c + e, 2 * ND)] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+  for (int j = 0; j < NK; ++j) {
+    const int x = threadIdx.x + j * T, t = x / (2 * D) * 16 + x % 16;
+    k[j] = load16(src_k, (t - at) * (2 * D) + x / 16 % (D / 8) * 16);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int x = threadIdx.x + j * T, t = x / (2 * D) * 32 + value_token(x / (D / 2) % 4, e);
+      v[j][e] = load4(src_v, (t - at) * (2 * D) + x % (D / 2) * 4);
+    }
+#pragma unroll
+  for (int j = 0; j < NK; ++j) {
+    const int x = threadIdx.x + j * T, t = x / (2 * D) * 16 + x % 16;
+    if (t >= at && t < end) *reinterpret_cast<uint4*>(k_tail + k_fp_index(t, x / 16 % (D / 8) * 8, ND)) = k[j];
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int x = threadIdx.x + j * T, a = x / (D / 2) % 4, t0 = x / (2 * D) * 32 + 4 * a;      // tokens t0 .. t0 + 3, t0 + 16 .. t0 + 19
+    if (t0 >= end || t0 + 19 < at) continue;
+    uint16_t* to = v_tail + v_fp_index(t0, x % (D / 2) * 2, 2 * ND);     // those of c, and behind them of c + 1
+    if (t0 >= at && t0 + 19 < end) {
+      auto piece = [&](uint32_t sel) {
+        return make_uint4(__builtin_amdgcn_perm(v[j][1], v[j][0], sel), __builtin_amdgcn_perm(v[j][3], v[j][2], sel),
+                          __builtin_amdgcn_perm(v[j][5], v[j][4], sel), __builtin_amdgcn_perm(v[j][7], v[j][6], sel));
+      };
+      reinterpret_cast<uint4*>(to)[0] = piece(0x05040100);
+      reinterpret_cast<uint4*>(to)[1] = piece(0x07060302);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int t = t0 + value_token(0, e);
+        if (t < at || t >= end) continue;
+        to[e] = (uint16_t)v[j][e];
+        to[e + 8] = (uint16_t)(v[j][e] >> 16);
+      }
+    }
   }
 }
 

@@ -45,6 +45,20 @@ def test_the_state_does_not_depend_on_the_calls(d, G, dtype):
         oracle.check(cache)
 
 
+@pytest.mark.parametrize("d,G,dtype", CASES)
+def test_one_append_to_rows_in_every_state(d, G, dtype):
+    """Rows whose tail is empty, begun or nearly full take no token, stay within the block, fill it up, or go on behind it, and one
+    reaches the capacity, all in one call."""
+    takes = lambda held: sorted({0, 1, G - held - 1, G - held, G - held + 1, 2 * G - held, 2 * G + 21 - held})
+    pairs = [(n, x) for n in (0, 1, 19, G - 1, G, 2 * G - 7) for x in takes(n % G)] + [(G + 9, 3 * G - 9)]
+    cache, oracle = build(15, len(pairs), 1, 1, d, G, dtype, [n for n, _ in pairs], capacity=4 * G)
+    new = [x for _, x in pairs]
+    K, V = (U.rows(17 + i, len(pairs), 1, max(new), d, dtype) for i in range(2))
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), new)
+    oracle.append(K, V, new)
+    oracle.check(cache)
+
+
 def test_more_rows_than_travel_in_a_launch():
     rng = np.random.default_rng(3)
     lengths = [int(x) for x in rng.integers(0, 100, 300)]
