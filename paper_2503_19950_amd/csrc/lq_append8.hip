@@ -18,6 +18,7 @@ namespace lq {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int WAVES = 4;
 
 struct Append8Params {
@@ -70,11 +71,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int byte
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
 }
 __device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0); }
-__device__ __forceinline__ uint4 load16(__amdgpu_buffer_rsrc_t rs, int off) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
-  return make_uint4(x[0], x[1], x[2], x[3]);
-}
+__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0); }
 
 // token within its unit of 32 at position e of the eight that lane row a holds: 16 b + 4 a + e % 4, b = e / 4
 __device__ __forceinline__ int value_token(int a, int e) { return 16 * (e >> 2) + 4 * a + (e & 3); }
@@ -204,7 +201,7 @@ __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params
   const int end = at + left;
   const __amdgpu_buffer_rsrc_t src_k = buffer(k_new + (int64_t)from * D, left * (2 * D)), src_v = buffer(v_new + (int64_t)from * D, left * (2 * D));
   constexpr int T = 64 * WAVES, NK = (G * D / 8 + T - 1) / T, NV = (G * D / 16 + T - 1) / T;
-  uint4 k[NK];
+  u32x4 k[NK];
   uint32_t v[NV][8];
 #pragma unroll
   for (int j = 0; j < NK; ++j) {
@@ -221,7 +218,7 @@ __global__ void __launch_bounds__(64 * WAVES) append8_kernel(const Append8Params
 #pragma unroll
   for (int j = 0; j < NK; ++j) {
     const int x = threadIdx.x + j * T, t = x / (2 * D) * 16 + x % 16;
-    if (t >= at && t < end) *reinterpret_cast<uint4*>(k_tail + k_fp_index(t, x / 16 % (D / 8) * 8, ND)) = k[j];
+    if (t >= at && t < end) *reinterpret_cast<u32x4*>(k_tail + k_fp_index(t, x / 16 % (D / 8) * 8, ND)) = k[j];
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -261,6 +258,22 @@ __global__ void __launch_bounds__(64 * WAVES) read8_kernel(const Read8Params P, 
   auto wanted = [&](int t) { return t >= P.t0 && t < end; };
   uint16_t* k_out = P.k_out + ((int64_t)bh * P.n - P.t0) * D;
   uint16_t* v_out = P.v_out + ((int64_t)bh * P.n - P.t0) * D;
+  // The rows of a unit are put together in LDS, a wavefront for itself, so that a store covers 1 KB of output in one
+  // stretch: stored from the lanes that convert them (64 bytes of a row at a time, values 4 bytes a lane) 131072 tokens x
+  // 8 heads took 208 us instead of 143, and a tail of 127 rows x 64 slices 11.1 instead of 4.7.
+  constexpr int PITCH = 2 * D + 16, CHUNKS = D / 8;          // bytes of a row, 16-byte pieces of it
+  __shared__ __align__(16) unsigned char stage[WAVES][32 * PITCH];
+  unsigned char* mine = stage[wave];
+  auto flush = [&](uint16_t* out) {
+    wave_lds_order();
+#pragma unroll
+    for (int x = 0; x < 32 * CHUNKS / 64; ++x) {
+      const int i = lane + 64 * x, t = i / CHUNKS, c = i % CHUNKS;
+      const uint4 y = *reinterpret_cast<const uint4*>(mine + t * PITCH + 16 * c);
+      if (wanted(32 * unit + t)) *reinterpret_cast<uint4*>(out + (int64_t)(32 * unit + t) * D + 8 * c) = y;
+    }
+    wave_lds_order();
+  };
   if (32 * unit < full) {
     const int64_t slice = ((int64_t)bh * P.cap + 32 * (int64_t)unit) * D;
     const int64_t block = (int64_t)bh * (P.cap >> P.log_g) + (32 * unit >> P.log_g);
@@ -275,22 +288,6 @@ __global__ void __launch_bounds__(64 * WAVES) read8_kernel(const Read8Params P, 
       for (int nd = 0; nd < ND; ++nd)
         v[nd] = *reinterpret_cast<const uint4*>(P.v_codes + slice + nd * 1024 + (16 * (lane / 16) + cc) * 16);
     const float sk = P.k_scale[block], sv = P.v_scale[block];
-    // The rows of a unit are put together in LDS, a wavefront for itself, so that a store covers 1 KB of output in one
-    // stretch: stored from the lanes that convert them (64 bytes of a row at a time, values 4 bytes a lane) 131072 tokens x
-    // 8 heads took 208 us instead of 143.
-    constexpr int PITCH = 2 * D + 16, CHUNKS = D / 8;          // bytes of a row, 16-byte pieces of it
-    __shared__ __align__(16) unsigned char stage[WAVES][32 * PITCH];
-    unsigned char* mine = stage[wave];
-    auto flush = [&](uint16_t* out) {
-      wave_lds_order();
-#pragma unroll
-      for (int x = 0; x < 32 * CHUNKS / 64; ++x) {
-        const int i = lane + 64 * x, t = i / CHUNKS, c = i % CHUNKS;
-        const uint4 y = *reinterpret_cast<const uint4*>(mine + t * PITCH + 16 * c);
-        if (wanted(32 * unit + t)) *reinterpret_cast<uint4*>(out + (int64_t)(32 * unit + t) * D + 8 * c) = y;
-      }
-      wave_lds_order();
-    };
     if (P.k_out) {
 #pragma unroll
       for (int nd = 0; nd < ND; ++nd) {
@@ -325,19 +322,33 @@ __global__ void __launch_bounds__(64 * WAVES) read8_kernel(const Read8Params P, 
     }
     return;
   }
-  const uint16_t* k_tail = P.k_tail + ((int64_t)bh << P.log_g) * D;
-  const uint16_t* v_tail = P.v_tail + ((int64_t)bh << P.log_g) * D;
-  for (int x = lane; x < 32 * (D / 8); x += 64) {
-    const int t = 32 * unit + x / (D / 8), c = x % (D / 8) * 8;
-    if (!wanted(t)) continue;
-    if (P.k_out) *reinterpret_cast<uint4*>(k_out + (int64_t)t * D + c) = *reinterpret_cast<const uint4*>(k_tail + k_fp_index(t - full, c, ND));
-    if (P.v_out) {
-      uint32_t w[4];
+  // the tail: rows of keys 16 bytes a lane, values as two channels of eight tokens; lanes whose rows are not there read nothing
+  const int64_t tail = (((int64_t)bh << P.log_g) + (32 * unit - full)) * D;
+  const int live = end - 32 * unit, nothing = 64 * D;
+  const __amdgpu_buffer_rsrc_t k_tail = buffer(P.k_tail + tail, 64 * D), v_tail = buffer(P.v_tail + tail, 64 * D);
+  u32x4 k[2 * ND], v[2 * ND];
+  if (P.k_out)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        w[e] = (uint32_t)v_tail[v_fp_index(t - full, c + 2 * e, 2 * ND)] | ((uint32_t)v_tail[v_fp_index(t - full, c + 2 * e + 1, 2 * ND)] << 16);
-      *reinterpret_cast<uint4*>(v_out + (int64_t)t * D + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int x = 0; x < 2 * ND; ++x) k[x] = load16(k_tail, 16 * (x / ND) + lane % 16 < live ? x * 1024 + lane * 16 : nothing);
+  if (P.v_out)
+#pragma unroll
+    for (int x = 0; x < 2 * ND; ++x)
+      v[x] = load16(v_tail, 4 * (lane / 16) < live ? (int)v_fp_index(4 * (lane / 16), 32 * (x / 2) + 2 * (lane % 16) + x % 2, 2 * ND) * 2 : nothing);
+  if (P.k_out) {
+#pragma unroll
+    for (int x = 0; x < 2 * ND; ++x)
+      *reinterpret_cast<u32x4*>(mine + (16 * (x / ND) + lane % 16) * PITCH + 2 * (32 * (x % ND) + 8 * (lane / 16))) = k[x];
+    flush(k_out);
+  }
+  if (P.v_out) {
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        *reinterpret_cast<uint32_t*>(mine + value_token(lane / 16, e) * PITCH + 2 * (32 * nd + 2 * (lane % 16))) =
+            __builtin_amdgcn_perm(v[2 * nd + 1][e / 2], v[2 * nd][e / 2], e & 1 ? 0x07060302 : 0x05040100);
     }
+    flush(v_out);
   }
 }
 
