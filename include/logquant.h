@@ -348,8 +348,11 @@ lq_status logquant_decode_plan_seq(const lq_config *cfg, const int32_t *n_fp, co
  * Lengths are per batch row, as for lq_cache_seq: n is a HOST array of B entries, owned by
  * the caller and updated by the calls; a row may be empty.  seq_state is DEVICE scratch
  * (logquant_sizes8) through which calls hand the counts to their kernels; a cache serves
- * one stream at a time.  DEVICE buffers that a call reads or writes start at a multiple of
- * 16 bytes (else LQ_ERR_SHAPE).  Errors are detected before anything is launched or
+ * one stream at a time.  A call recorded into a HIP graph keeps the counts of the recording:
+ * replayed, it reads or writes the same places again (an append that goes on behind a block
+ * with rows in the tail takes their place there, so that its replays find others).
+ * DEVICE buffers that a call reads or writes start at a multiple of 16 bytes (else
+ * LQ_ERR_SHAPE).  Errors are detected before anything is launched or
  * changed. */
 typedef struct {
   int32_t B;           /* batch rows                                                   */
