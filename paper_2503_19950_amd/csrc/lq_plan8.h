@@ -9,19 +9,17 @@ namespace lq {
 // Parts of an item of u units when none may be larger than `most`.  Up to 20 units, five to a wavefront, it stays whole
 // (512 tokens x 8 kv heads: whole 4.9 us, 2 parts 6.4, 4 parts 6.0; 1024 tokens: 6.9, 7.2, 6.4 and 8 parts 5.8).
 constexpr int WHOLE8 = 20;
-inline int parts_of(int64_t u, int64_t most) { return u > most && u > WHOLE8 ? (int)((u + most - 1) / most) : 1; }
+inline int parts_of(int u, int most) { return u > most && u > WHOLE8 ? (u + most - 1) / most : 1; }
 
-// The largest load of a compute unit, in units of work, when items over a `whole`-th of it are split into parts of a
-// `shares`-th: the 256 largest workgroups one each, the others from the largest down to the least loaded ones (beyond 512:
-// evenly).
-inline int64_t largest_load(int rows, const int64_t* units, int per_row, int64_t work, int shares, int whole) {
+// The largest load of a compute unit, in units of work, when items of more than `over` units are split into parts of at most
+// `most`: the 256 largest workgroups one each, the others from the largest down to the least loaded ones (beyond 512: evenly).
+inline int64_t largest_load(const Row8* r, int rows, int per_row, int most, int over) {
   constexpr int CUS = 256;
   struct Class { int64_t size, n; };
-  Class few[ROWS_IN_ARGS];
-  const int64_t most = std::max<int64_t>((work + shares - 1) / shares, 4);
+  Class few[CUS];
   for (int b = 0; b < rows; ++b) {
-    const int parts = units[b] * whole <= work ? 1 : parts_of(units[b], most);
-    few[b] = Class{(units[b] + parts - 1) / parts, (int64_t)parts * per_row};
+    const int u = r[b].x, parts = u > over ? parts_of(u, most) : 1;
+    few[b] = Class{(u + parts - 1) / parts, (int64_t)parts * per_row};
   }
   std::sort(few, few + rows, [](const Class& x, const Class& y) { return x.size > y.size; });
   int64_t load = few[0].size, left = CUS;
@@ -60,14 +58,14 @@ inline int64_t largest_load(int rows, const int64_t* units, int per_row, int64_t
 //  - a few items more than 256: rows for 256 stay whole, the rest is split into 256 (260 items 59.5 -> 50.9; 304 items
 //    64.4 -> 56.9; from 340 on the reserve covers the second item of a compute unit).
 // Rows of different lengths:
-//  - up to 256 items: the smallest `most` that makes no more than 256 parts (16 rows of up to 8000 x 8 kv heads 36.1 -> 31.9;
-//    4 rows of up to 30000 34.8 -> 28.7), if that is within 1.5 of the even share.
-//  - else what is over a 200th of all work is split into parts of a 256th, or, of up to 256 items, over a 300th into parts of
-//    a 384th where that loads the compute units more evenly (45 rows of up to 24597 x 4 kv heads 132 -> 108, but 1 of 65536
-//    and 29 of 512 x 8: 33.6 and 40.0).  Few and large workgroups, of 8 or 16 wavefronts, the longest first, leave the balance
-//    to their placement (64 rows of up to 4096 x 8 kv heads: 4 wavefronts 54.5, 8 54.6, 16 49.5; 100 of up to 4000: 79.9, 75.8,
-//    76.4; 30 of up to 9000, d = 96: 43.0, 43.6, 47.0), unless they are small (200 rows of up to 2000, 31 units each: 4
-//    wavefronts 75.6, 16 84.6) or many, which balance by their number.
+//  - up to 256 items: parts no larger than it takes for 256 of them, if that is within 1.25 of the even share (4 rows of up to
+//    30000 x 8 kv heads 29.0; 512 parts 30.4; 31 rows of 4000 to 5500: 54.2 and 57.8), else for 512, two to a compute unit (24
+//    rows of up to 12000: 256 parts 66.8, 512 58.8; 16 of up to 8000: 32.1 and 30.5; 20 of up to 20000, d = 64: 54.3 and 43.6),
+//    unless the next rule loads the compute units more evenly (1 of 65536 and 29 of 512: 40.9, with it 33.6).
+//  - what is over a 200th of all work is split into parts of a 256th.  Few and large workgroups, of 8 or 16 wavefronts, the
+//    longest first, leave the balance to their placement (64 rows of up to 4096 x 8 kv heads: 4 wavefronts 54.5, 8 54.6, 16 49.5;
+//    100 of up to 4000: 79.9, 75.8, 76.4), unless they are small (200 rows of up to 2000, 31 units each: 4 wavefronts 75.6, 16
+//    84.6) or many, which balance by their number.
 inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows, Plan8* p) {
   constexpr int CUS = 256, LEAST = 4;
   int64_t tokens = 0;
@@ -97,35 +95,38 @@ inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows,
       }
     }
   } else {
-    int64_t work = 0, longest = LEAST, most = 0;
+    int64_t work = 0;
+    int longest = LEAST;
     for (Row8* r = first; r != last; ++r) {
-      const int64_t u = r->x;
-      work += u * per_row;
-      longest = std::max(longest, u);
+      work += (int64_t)r->x * per_row;
+      longest = std::max(longest, r->x);
     }
+    // parts of a 256th of what is over a 200th
+    const int even = (int)std::max<int64_t>((work + CUS - 1) / CUS, LEAST);
+    int most = even, over = (int)(work / 200);
+    bool by_share = true;                              // this rule
     if (items <= CUS) {
-      int64_t lo = LEAST, hi = longest;
-      while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        int64_t n = 0;
-        for (Row8* r = first; r != last; ++r) n += parts_of(r->x, mid);
-        if (n * per_row <= CUS) hi = mid; else lo = mid + 1;
+      auto smallest = [&](int limit) {                 // size of parts with which there are no more than `limit`, of an item 256
+        int lo = std::max(LEAST, (longest + 255) / 256), hi = longest;
+        while (lo < hi) {
+          const int mid = lo + (hi - lo) / 2;
+          int64_t n = 0;
+          for (Row8* r = first; r != last; ++r) n += parts_of(r->x, mid);
+          if (n * per_row <= limit) hi = mid; else lo = mid + 1;
+        }
+        return lo;
+      };
+      const int one = smallest(CUS);
+      by_share = one > LEAST && 4 * (int64_t)one * CUS > 5 * work;
+      const int two = by_share ? smallest(2 * CUS) : one;
+      if (!by_share || largest_load(first, n_rows, per_row, two, 0) <= largest_load(first, n_rows, per_row, even, over)) {
+        most = two;
+        over = 0;
+        by_share = false;
       }
-      if (lo == LEAST || 2 * lo * CUS <= 3 * work) most = lo;
     }
-    if (most) {
-      for (Row8* r = first; r != last; ++r) r->parts = parts_of(r->x, most);
-    } else {
-      int shares = CUS, whole = 200;
-      if (items <= CUS && n_rows <= ROWS_IN_ARGS) {
-        int64_t u[ROWS_IN_ARGS];
-        for (int b = 0; b < n_rows; ++b) u[b] = rows[b].x;
-        if (largest_load(n_rows, u, per_row, work, 384, 300) < largest_load(n_rows, u, per_row, work, CUS, 200)) shares = 384, whole = 300;
-      }
-      most = std::max<int64_t>((work + shares - 1) / shares, LEAST);
-      for (Row8* r = first; r != last; ++r) r->parts = (int64_t)r->x * whole <= work ? 1 : parts_of(r->x, most);
-      if (items <= 1024 && work >= 24 * items) p->waves = items <= CUS ? 8 : 16;
-    }
+    for (Row8* r = first; r != last; ++r) r->parts = r->x > over ? parts_of(r->x, most) : 1;
+    if (by_share && items <= 1024 && work >= 24 * items) p->waves = items <= CUS ? 8 : 16;
     // (by work, not by tokens: what is split has to come first)
     std::sort(first, last, [](const Row8& x, const Row8& y) { return x.x > y.x; });
   }
