@@ -5,17 +5,19 @@
 // head as the columns of one operand:
 //   S^T = K Q^T   codes of keys, e4m3, which fp16 and bf16 hold exactly, against q as it came; the scale of a block is one
 //                 factor of the fp32 logits of its tokens
-//   O^T = V^T P^T codes of values as fp16 against the probabilities, rounded to fp16; the scale of a block is one factor of
-//                 the fp32 sum over a unit of 32 tokens, which is then added to the running sums
+//   O^T = V^T P^T codes of values as fp16 against the probabilities as the sum of two fp16 operands; the scale of a block is one
+//                 factor of the fp32 sum over a unit of 32 tokens, which is then added to the running sums
 // A lane of S^T holds four tokens of one head, which are the elements it owes to P^T (tokens permuted inside a unit, as they
 // are stored), and the result of O^T has the heads in the same lanes: nothing but the maximum crosses lanes.
 // Probabilities are 2^(s' - m + 10) with s' = s log2(e) and m the largest s' when it was last looked up, at most 5 behind:
-// they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  Their rounding to fp16 moves an output by
-// 1.4e-4 of itself, which disappears in the rounding of a bf16 output (1.7e-3), but not in that of an fp16 one (2.1e-4; together
-// 3.0e-4 at 512 tokens): for fp16 caches what the rounding left is a second operand (8 rows of 8192 tokens 27.1 us with and
-// without).  The sum of the probabilities is kept in fp32, before any rounding.
+// they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  The second operand is what the rounding of
+// the first one left, so that a probability is held to 22 bits.  Without it an output moves by 1.4e-4 of itself, which carries
+// one bf16 output in twenty over a border of its own rounding: the outputs were 7.3e-4 (2-norm; 16 rows x 32 heads x 32768,
+// d = 96) and 7.1e-4 (8 kv heads, 520 tokens) from those with probabilities in fp32, now 1.6e-4 and 5.5e-5.  It costs nothing
+// with up to 16 heads in a workgroup (those 16 rows 520.5 us with and without, 131072 tokens x 8 kv heads 49.9) and up to 5 % with
+// more (8 rows of 20000, 24 heads 19.9 -> 20.6 us).  The sum of the probabilities is kept in fp32, before any rounding.
 //
-// Bound by the bytes of the codes.  A unit of d = 128 (8 KB) costs a wavefront about 200 vector and 16 to 24 matrix
+// Bound by the bytes of the codes.  A unit of d = 128 (8 KB) costs a wavefront about 200 vector and 24 matrix
 // instructions, a quarter of what a compute unit has time for while its share of them arrives.  Keys of the next unit are
 // loaded while the values of this one are used, in the same registers, so that 4 wavefronts fit a SIMD; one to three units
 // more in flight brought nothing.  131072 tokens x 8 kv heads, bf16, 269 MB: 48.9 us, 5.5 TB/s; of these 1.7 us until the first
@@ -96,17 +98,15 @@ __device__ __forceinline__ uint32_t pair_as(float a, float b) {
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), half2v));
 }
 
-// eight probabilities as an operand, and what their rounding left as a second one
+// eight probabilities as an operand, and what is left of them without it (exact)
 template <bool BF16>
 __device__ __forceinline__ u32x4 operand(const float* p) {
   return u32x4{pair_as<BF16>(p[0], p[1]), pair_as<BF16>(p[2], p[3]), pair_as<BF16>(p[4], p[5]), pair_as<BF16>(p[6], p[7])};
 }
 template <bool BF16>
-__device__ __forceinline__ u32x4 rest_of(const float* p, u32x4 op) {
-  float r[8];
+__device__ __forceinline__ void take(float* p, u32x4 op) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = p[e] - t2f<BF16>((uint16_t)(op[e / 2] >> (16 * (e & 1))));
-  return operand<BF16>(r);
+  for (int e = 0; e < 8; ++e) p[e] -= t2f<BF16>((uint16_t)(op[e / 2] >> (16 * (e & 1))));
 }
 
 // over the four lanes of a head (lane % 16)
@@ -355,11 +355,12 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
           p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m[x]));
           l[x] += p[e];
         }
-        const u32x4 pb = operand<BF16>(p), pr = rest_of<BF16>(p, pb);     // (a bf16 operand keeps 8 bits, an fp16 one 11)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          acc[x][t] = mfma<BF16>(vt[t], pb, acc[x][t]);
-          acc[x][t] = mfma<BF16>(vt[t], pr, acc[x][t]);
+        for (int y = 0; y < (BF16 ? 3 : 2); ++y) {     // a bf16 operand keeps 8 bits, an fp16 one 11
+          const u32x4 pb = operand<BF16>(p);
+          take<BF16>(p, pb);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[x][t] = mfma<BF16>(vt[t], pb, acc[x][t]);
         }
       }
     }
@@ -402,7 +403,8 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
         l[x] += p[e];
       }
       pb[x] = operand<false>(p);
-      if constexpr (!BF16) pr[x] = rest_of<false>(p, pb[x]);
+      take<false>(p, pb[x]);
+      pr[x] = operand<false>(p);
     }
 #pragma unroll
     for (int nd = 0; nd < ND; ++nd) {
@@ -410,11 +412,7 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
       const u32x4 v0 = codes_as<false>(v[nd][0], v[nd][1]), v1 = codes_as<false>(v[nd][2], v[nd][3]);
 #pragma unroll
       for (int x = 0; x < SETS; ++x) {
-        f32x4 o0 = mfma<false>(v0, pb[x], zero), o1 = mfma<false>(v1, pb[x], zero);
-        if constexpr (!BF16) {
-          o0 = mfma<false>(v0, pr[x], o0);
-          o1 = mfma<false>(v1, pr[x], o1);
-        }
+        const f32x4 o0 = mfma<false>(v0, pr[x], mfma<false>(v0, pb[x], zero)), o1 = mfma<false>(v1, pr[x], mfma<false>(v1, pb[x], zero));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           acc[x][2 * nd][e] = fmaf(o0[e], f, acc[x][2 * nd][e]);
