@@ -9,8 +9,10 @@
 //                 factor of the fp32 sum over a unit of 32 tokens, which is then added to the running sums
 // A lane of S^T holds four tokens of one head, which are the elements it owes to P^T (tokens permuted inside a unit, as they
 // are stored), and the result of O^T has the heads in the same lanes: nothing but the maximum crosses lanes.
-// Probabilities are 2^(s' - m + 10) with s' = s log2(e) and m the largest s' when it was last looked up, at most 5 behind:
-// they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  The second operand is what the rounding of
+// Probabilities are 2^(s' - m) with s' = s log2(e) and m the largest s' when it was last looked up, at most 5 behind, less 10:
+// they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  s' is rounded once, as m was, before they
+// are subtracted, and m is no further from it than fp32 can tell (`reference`): from |s'| = 2^24 on, with 10 - m rounded and s'
+// not, probabilities were off by powers of two or infinite (a token of 3000 s in q and k, d = 128: NaN).  The second operand is what the rounding of
 // the first one left, so that a probability is held to 22 bits.  Without it an output moves by 1.4e-4 of itself, which carries
 // one bf16 output in twenty over a border of its own rounding: the outputs were 7.3e-4 (2-norm; 16 rows x 32 heads x 32768,
 // d = 96) and 7.1e-4 (8 kv heads, 520 tokens) from those with probabilities in fp32, now 1.6e-4 and 5.5e-5.  It costs nothing
@@ -127,6 +129,18 @@ __device__ __forceinline__ float head_sum(float v) {
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// A logit, rounded: left to itself the compiler may join it to the subtraction behind it, where the reference was rounded.
+__device__ __forceinline__ float product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+// What is subtracted from logits whose largest is t: t - BIAS, but never so far below t (where fp32 is coarser than that, from
+// 2^27 on) that a probability would leave fp16.
+__device__ __forceinline__ float reference(float t) {
+  const float m = t - BIAS;
+  return t - m > BIAS + SLACK ? t : m;
+}
+
 __device__ __forceinline__ float weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
 
 // SETS: sets of 16 query heads, the columns of an operand, that share the loads and the converted codes.
@@ -227,10 +241,10 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
     for (int t = 0; t < NT; ++t) acc[x][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // a lane's largest logit of a unit: when it is over the reference by more than SLACK anywhere, a new reference
+  // a lane's largest logit of a unit: when it is over the largest so far by more than SLACK anywhere, a new reference
   auto look_up = [&](int x, float top) {
-    if (__any(top > m[x] + SLACK)) {
-      const float now = fmaxf(m[x], head_max(top)), f = weight(m[x], now);
+    if (__any(top - m[x] > BIAS + SLACK)) {
+      const float now = fmaxf(m[x], reference(head_max(top))), f = weight(m[x], now);
       m[x] = now;
       l[x] *= f;
 #pragma unroll
@@ -345,14 +359,14 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
         float z[8], top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          z[e] = 16 * (e / 4) + 4 * a + e % 4 < live ? (e < 4 ? s0[e] : s1[e - 4]) * P.scale : -INFINITY;
+          z[e] = 16 * (e / 4) + 4 * a + e % 4 < live ? product(e < 4 ? s0[e] : s1[e - 4], P.scale) : -INFINITY;
           top = fmaxf(top, z[e]);
         }
         look_up(x, top);
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(z[e] + (BIAS - m[x]));
+          p[e] = __builtin_amdgcn_exp2f(z[e] - m[x]);
           l[x] += p[e];
         }
 #pragma unroll
@@ -394,12 +408,17 @@ __global__ void __launch_bounds__(64 * NW, SETS == 1 ? 4 : 2) attn8_kernel(const
     u32x4 pb[SETS], pr[SETS];
 #pragma unroll
     for (int x = 0; x < SETS; ++x) {
-      const f32x4 y0 = s0[x], y1 = s1[x];
-      look_up(x, fmaxf(fmaxf(fmaxf(y0[0], y0[1]), fmaxf(y0[2], y0[3])), fmaxf(fmaxf(y1[0], y1[1]), fmaxf(y1[2], y1[3]))) * c);
+      float z[8], top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        z[e] = product(e < 4 ? s0[x][e] : s1[x][e - 4], c);
+        top = fmaxf(top, z[e]);
+      }
+      look_up(x, top);
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(e < 4 ? y0[e] : y1[e - 4], c, BIAS - m[x]));
+        p[e] = __builtin_amdgcn_exp2f(z[e] - m[x]);
         l[x] += p[e];
       }
       pb[x] = operand<false>(p);
