@@ -391,8 +391,10 @@ lq_status logquant_workspace_init8(const lq_config8 *cfg, void *workspace, void 
  * LQ_ERR_SHAPE for n_max < 1 or an n_new outside its range, LQ_ERR_CAPACITY if a row would
  * pass `capacity`.  On success n[b] += n_new[b].
  * The caller may set n[b] back to drop tokens (a draft that was rejected) as far as the tail
- * still holds the rows of the block that the new count ends in: that of the last n % G rows,
- * or, when n % G == 0 after a call that filled up a block of the tail, that block's. */
+ * still holds the rows of the block that the new count ends in.  It holds the last n % G rows.
+ * When n % G == 0 it holds all rows of the last block if that had rows in the tail before the
+ * call (append or step) that filled it up, and the call brought the row no token behind it;
+ * of a block that one call brings whole, or fills up and goes on, it does not. */
 lq_status logquant_append8(const lq_config8 *cfg, lq_cache8 *cache, const void *k_new,
                            const void *v_new, const int32_t *n_new, int32_t n_max, void *stream);
 
