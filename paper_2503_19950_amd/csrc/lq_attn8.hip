@@ -588,7 +588,8 @@ hipError_t attn8(const Shape8& s, const Attn8Params& p, const Rows8<MODE>& rows,
   auto with_type = [&](auto bf16) {
     const std::integral_constant<int, 1> one;
     if (plan.hb > 16) return with(bf16, std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-    if (plan.waves == 16) return with(bf16, std::integral_constant<int, 16>{}, one);
+    if constexpr (MODE == ROWS_LISTED)                 // (plan8 has no 16 for rows that are alike)
+      if (plan.waves == 16) return with(bf16, std::integral_constant<int, 16>{}, one);
     if (plan.waves == 8) return with(bf16, std::integral_constant<int, 8>{}, one);
     with(bf16, std::integral_constant<int, 4>{}, one);
   };

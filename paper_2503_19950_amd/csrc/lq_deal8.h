@@ -82,10 +82,12 @@ LQ8_HD int turned8(const Part8& p, int i, int turn) {
 
 // A workspace: the counters of the items, each item's (one for all its parts, others for sixteen of them each) in a cache line,
 // then room for the partial results of the workgroups that share an item (they come first in the grid), and as much again for
-// those of sixteen joined.
+// those of sixteen joined.  No plan has more than MAX_PARTS8:
+// rows that are alike are split into 256 workgroups at most, rows of different lengths into 512 or, what is over a 200th of the
+// work (fewer than 200 items), into parts of a 256th, at most 256 and one more for each item.
 constexpr int FAN8 = 16;           // parts joined at a time where there are many
 constexpr int CTR8 = 32;           // ints from one counter to the next
-constexpr int MAX_PARTS8 = 1024;
+constexpr int MAX_PARTS8 = 512;
 // Head groups of a kv head.  More than 16 heads are two sets in one workgroup, which read the cache once, or two workgroups,
 // which share the join's work: the former in launches that read 24 MB or more.
 inline int head_groups8(const Shape8& s, bool large) { return (s.gh + (large ? 31 : 15)) / (large ? 32 : 16); }
