@@ -18,7 +18,6 @@ namespace lq {
 
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int WAVES = 4;
 
 struct Append8Params {
@@ -67,11 +66,7 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {   // reads beyond it: zeros
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
-}
 __device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0); }
-__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0); }
 
 // token within its unit of 32 at position e of the eight that lane row a holds: 16 b + 4 a + e % 4, b = e / 4
 __device__ __forceinline__ int value_token(int a, int e) { return 16 * (e >> 2) + 4 * a + (e & 3); }

@@ -44,7 +44,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float BIAS = 10.f, SLACK = 5.f;
@@ -64,13 +63,6 @@ struct Attn8Params {
   int B, Hkv, gh, groups, hb, log_g, cap;
   Row8 same;                                 // ROWS_SAME: every row's entry
 };
-
-__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t rs, int off) {
-  return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
-}
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
-}
 
 // eight codes as an operand of T
 template <bool BF16>

@@ -1,8 +1,15 @@
-// Quantizer of the 8-bit cache, on the 16-bit patterns of pairs of values.
+// What the kernels of the 8-bit cache share: loads, and the quantizer, on the 16-bit patterns of pairs of values.
 #pragma once
 #include "lq_device.h"
 
 namespace lq {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {   // reads beyond it: zeros
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0); }
 
 // Magnitudes of a pair of values of T order like their 15 low bits as integers.
 __device__ __forceinline__ uint32_t max_pair(uint32_t m, uint32_t x) {
