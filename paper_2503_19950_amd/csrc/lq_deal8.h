@@ -89,7 +89,10 @@ constexpr int FAN8 = 16;           // parts joined at a time where there are man
 constexpr int CTR8 = 32;           // ints from one counter to the next
 constexpr int MAX_PARTS8 = 512;
 // Head groups of a kv head.  More than 16 heads are two sets in one workgroup, which read the cache once, or two workgroups,
-// which share the join's work: the former in launches that read 24 MB or more.
+// which share the join's work: the former in launches that read 24 MB or more, where rows and kv heads are many (24 heads a kv
+// head: 8 rows of 8192 x 8 kv heads, 134 MB, 36.2 us as two workgroups, 30.3 as two sets; 16 rows of 3000 x 4, 49 MB, 18.0 and
+// 17.1; 1 row of 8192 x 8, 17 MB, 12.2 and 15.4).  A single kv head in many parts, whose join is long, would do better as
+// two workgroups at any size (524288 tokens, 134 MB, 41.2 and 44.3; 94000 tokens, 24 MB, 17.7 and 22.1).
 inline int head_groups8(const Shape8& s, bool large) { return (s.gh + (large ? 31 : 15)) / (large ? 32 : 16); }
 inline size_t counter_bytes8(const Shape8& s) { return (size_t)s.B * s.Hkv * head_groups8(s, false) * CTR8 * sizeof(int); }
 inline int partial_floats8(int hb, int d) { return hb * (d + 4); }   // o, then m and l, padded to 16 bytes

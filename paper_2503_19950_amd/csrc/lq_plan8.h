@@ -62,10 +62,13 @@ inline int64_t largest_load(const Row8* r, int rows, int per_row, int most, int 
 //    30000 x 8 kv heads 29.0; 512 parts 30.4; 31 rows of 4000 to 5500: 54.2 and 57.8), else for 512, two to a compute unit (24
 //    rows of up to 12000: 256 parts 66.8, 512 58.8; 16 of up to 8000: 32.1 and 30.5; 20 of up to 20000, d = 64: 54.3 and 43.6),
 //    unless the next rule loads the compute units more evenly (1 of 65536 and 29 of 512: 40.9, with it 33.6).
-//  - what is over a 200th of all work is split into parts of a 256th.  Few and large workgroups, of 8 or 16 wavefronts, the
-//    longest first, leave the balance to their placement (64 rows of up to 4096 x 8 kv heads: 4 wavefronts 54.5, 8 54.6, 16 49.5;
-//    100 of up to 4000: 79.9, 75.8, 76.4), unless they are small (200 rows of up to 2000, 31 units each: 4 wavefronts 75.6, 16
-//    84.6) or many, which balance by their number.
+//  - what is over a 200th of all work is split into parts of a 256th.  Few and large workgroups, of 8 wavefronts for up to 256 items
+//    and of 16 for up to 1024, the longest first, leave the balance to their placement, where items have 24 units on average.  With
+//    4, 8 and 16 wavefronts, items and average units in brackets, 8 kv heads: 64 rows of up to 4096 (512, 65) 55.0, 54.7, 49.6; 100 of
+//    up to 4000 (800, 64) 80.8, 77.1, 76.7; 100 of up to 3000 (800, 48) 62.0, 58.3, 60.3; 64 of up to 1500 (512, 24) 23.1, 23.3, 22.9;
+//    64 of up to 1000 (512, 17) 16.7, 17.2, 17.6.  Near 24 units many items would do better with fewer wavefronts (100 rows of up to
+//    2000, 800 items, 32 units: 43.8, 40.8, 45.3; 200 x 4 kv heads 46.4, 44.7, 48.8; 100 of up to 1500 33.8, 32.4, 37.2), as do
+//    more than 1024, which balance by their number (200 of up to 2000: 75.6 with 4, 84.6 with 16).
 inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows, Plan8* p) {
   constexpr int CUS = 256, LEAST = 4;
   int64_t tokens = 0;
