@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(64 * WAVES) read8_kernel(const Read8Params P, 
   uint16_t* v_out = P.v_out + ((int64_t)bh * P.n - P.t0) * D;
   // The rows of a unit are put together in LDS, a wavefront for itself, so that a store covers 1 KB of output in one
   // stretch: stored from the lanes that convert them (64 bytes of a row at a time, values 4 bytes a lane) 131072 tokens x
-  // 8 heads took 208 us instead of 143, and a tail of 127 rows x 64 slices 11.1 instead of 4.7.
+  // 8 heads took 208 us instead of 150, and a tail of 127 rows x 64 slices 11.1 instead of 4.7.
   constexpr int PITCH = 2 * D + 16, CHUNKS = D / 8;          // bytes of a row, 16-byte pieces of it
   __shared__ __align__(16) unsigned char stage[WAVES][32 * PITCH];
   unsigned char* mine = stage[wave];

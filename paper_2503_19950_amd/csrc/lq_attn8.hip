@@ -12,19 +12,21 @@
 // Probabilities are 2^(s' - m) with s' = s log2(e) and m the largest s' when it was last looked up, at most 5 behind, less 10:
 // they stay below 2^15, and one 2^-24 of the largest still is a normal fp16 number.  s' is rounded once, as m was, before they
 // are subtracted, and m is no further from it than fp32 can tell (`reference`): from |s'| = 2^24 on, with 10 - m rounded and s'
-// not, probabilities were off by powers of two or infinite (a token of 3000 s in q and k, d = 128: NaN).  The second operand is what the rounding of
-// the first one left, so that a probability is held to 22 bits.  Without it an output moves by 1.4e-4 of itself, which carries
-// one bf16 output in twenty over a border of its own rounding: the outputs were 7.3e-4 (2-norm; 16 rows x 32 heads x 32768,
-// d = 96) and 7.1e-4 (8 kv heads, 520 tokens) from those with probabilities in fp32, now 1.6e-4 and 5.5e-5.  It costs nothing
-// with up to 16 heads in a workgroup (those 16 rows 520.5 us with and without, 131072 tokens x 8 kv heads 49.9) and up to 5 % with
-// more (8 rows of 20000, 24 heads 19.9 -> 20.6 us).  The sum of the probabilities is kept in fp32, before any rounding.
+// not, probabilities were off by powers of two or infinite (a token of 3000s in q and k, d = 128: NaN).
+// The second operand is what the rounding of the first one left, so that a probability is held to 22 bits, or to 2^-35 of the
+// largest.  Without it an output moves by 1.4e-4 of itself, which carries one bf16 output in twenty over a border of its own
+// rounding: the outputs were 7.3e-4 (2-norm; 16 rows x 32 heads x 32768, d = 96) and 7.1e-4 (8 kv heads, 520 tokens) from those
+// with probabilities in fp32, now 1.6e-4 and 5.5e-5.  It costs nothing with up to 16 heads in a workgroup (those 16 rows 520.5 us
+// with and without, 131072 tokens x 8 kv heads 49.9) and up to 5 % with more (8 rows of 20000, 24 heads 19.9 -> 20.6 us).  The
+// tail's operands are of T, two of fp16 or three of bf16 (a step over 520 tokens 6.1 -> 6.4 us with the third).  The sum of the
+// probabilities is kept in fp32, before any rounding.
 //
 // Bound by the bytes of the codes.  A unit of d = 128 (8 KB) costs a wavefront about 200 vector and 24 matrix
 // instructions, a quarter of what a compute unit has time for while its share of them arrives.  Keys of the next unit are
 // loaded while the values of this one are used, in the same registers, so that 4 wavefronts fit a SIMD; one to three units
-// more in flight brought nothing.  131072 tokens x 8 kv heads, bf16, 269 MB: 48.9 us, 5.5 TB/s; of these 1.7 us until the first
+// more in flight brought nothing.  131072 tokens x 8 kv heads, bf16, 269 MB: 49.7 us, 5.4 TB/s; of these 1.7 us until the first
 // keys are there, 40.5 in the loop (6.6 TB/s), 3 between the first and the last wavefront to end, 3 to join 32 parts.
-// 16 rows x 32 heads x 32768, d = 96, 3.2 GB: 520 us, 6.2 TB/s, 0.97 of what a plain read reaches.
+// 16 rows x 32 heads x 32768, d = 96, 3.2 GB: 518 us, 6.2 TB/s, 0.97 of what a plain read reaches.
 //
 // Workgroups take items or parts of them (lq_plan8.h), their wavefronts unit by unit (lq_deal8.h).
 #include <type_traits>
