@@ -423,6 +423,159 @@ lq_status logquant_decode_step8(const lq_config8 *cfg, lq_cache8 *cache, const v
                                 const void *v_new, const void *q, float softmax_scale, void *out,
                                 void *workspace, void *stream);
 
+/* ---- Rotary positions ----------------------------------------------------------------
+ * Keys arrive position-encoded at every cache above (Sec. 2.4: what makes Eq. 3 apply).
+ * This is that encoding: the first `dims` channels of a row are pairs, and pair i of the
+ * row at position p turns by the angle a = p * freq[i]:
+ *   (x0, x1) -> factor * (x0 cos a - x1 sin a, x1 cos a + x0 sin a)
+ * the other channels stay.  Pairs are channels (i, i + dims/2), or (2i, 2i+1) with
+ * `interleaved`.  Angles are reduced in fp64, so far positions are as exact as near ones;
+ * a result is computed in fp32 and rounded to T once.  A negative position turns back. */
+typedef struct {
+  int32_t dims;          /* rotated channels, even, 2 .. d                               */
+  int32_t interleaved;   /* 0: pairs (i, i + dims/2); 1: pairs (2i, 2i+1)                */
+  float   factor;        /* on the rotated channels (attention scaling), 1: none         */
+  const double *freq;    /* DEVICE, dims/2 radians per position                          */
+} lq_rope;
+
+/* Frequencies (pure host arithmetic; freq: HOST, dims/2 entries): base^(-2i/dims), and
+ * for contexts longer than those trained on
+ *   stretch != 1, original == 0: divided by `stretch` (positions interpolated);
+ *   original > 0: by parts.  A pair that turns `fast` times or more in `original` tokens
+ *   stays, one that turns `slow` times or fewer is divided by `stretch`, and between them
+ *   w f + (1 - w) f / stretch with w = (turns - slow) / (fast - slow).
+ * LQ_ERR_SHAPE for an odd dims or one below 2, base or stretch not positive and finite,
+ * original negative, or original > 0 with fast <= slow. */
+lq_status logquant_rope_frequencies(int32_t dims, double base, double stretch, double original,
+                                    double slow, double fast, double *freq);
+
+/* Queries and keys turned by their positions, in one launch:
+ *   q, q_out : DEVICE [B][Hq][L][d] T      k, k_out : DEVICE [B][Hkv][L][d] T, row-major.
+ *   positions : DEVICE [B][L] int32; null: token t of every row is at position t.
+ * A pair of pointers may be null (not wanted); an output may be its input (in place) and
+ * must not overlap it otherwise.  d as for a cache.  LQ_ERR_SHAPE for a dimension below 1,
+ * dims odd or outside 2 .. d, a factor that is not finite, a tensor that does not start at
+ * a multiple of 16 bytes; LQ_ERR_UNSUPPORTED for B > 65535, another d, or 2^31 rows or more
+ * in a tensor. */
+lq_status logquant_rotate(const lq_rope *rope, int32_t B, int32_t L, int32_t Hq, int32_t Hkv,
+                          int32_t d, int32_t dtype, const int32_t *positions, const void *q,
+                          void *q_out, const void *k, void *k_out, void *stream);
+
+/* ---- Paged cache ---------------------------------------------------------------------
+ * A third kind of cache: every token in T, in pages of `page` tokens out of a pool that
+ * all rows share.  A table names the pages of a row in order, so rows need no room at
+ * their longest, rows may share the pages of a common prompt, and a row that gives up
+ * tokens (logquant_evict_paged) gives up pages.
+ *
+ * Layouts (kperm as above): the element (token t, channel c) of kv head h in page g,
+ * 0 <= t < page, lies at
+ *   k_pages  T    index (((((g*Hkv + h)*(page/16)) + t/16)*(d/32) + c/32)*64 + 16*((c%32)/8) + t%16)*8 + c%8
+ *   v_pages  T    index (((((g*Hkv + h)*(page/32)) + t/32)*(d/16) + c/16)*64 + 16*(k/8) + c%16)*8 + k%8,
+ *                 k = kperm(t % 32)
+ *   table    i32  index (half*B + b)*max_pages + j       page of tokens j*page .. j*page + page-1 of row b
+ *   weights  f32  index ((half*B + b)*Hkv + h)*max_pages*page + t      (if `weighted`)
+ * A row uses one half of table and weights, cur[b]; the other is where eviction puts it.
+ * Slots at and behind a row's length are neither written nor do they influence a result.
+ * A page that several rows name must be full of tokens that they share: a call that
+ * writes to it for two of them leaves either's.  An entry of the table that is outside
+ * 0 .. n_pages-1 is no page: its tokens get no attention and nothing is stored for them.
+ *
+ * n, cur and pages are HOST arrays, owned by the caller and, n and cur, updated by the
+ * calls; seq_state, streams, graphs (a recorded call keeps its counts, and reads table and
+ * weights as they are when it is replayed), alignment and errors are as for the 8-bit
+ * cache. */
+typedef struct {
+  int32_t B;           /* batch rows                                                   */
+  int32_t Hq;          /* query heads; query head h reads kv head h / (Hq/Hkv)         */
+  int32_t Hkv;         /* kv heads, Hq % Hkv == 0                                      */
+  int32_t d;           /* head dimension, one of 64, 96, 128                           */
+  int32_t page;        /* tokens of a page, 32/64/128                                  */
+  int32_t dtype;       /* lq_dtype                                                     */
+  int32_t n_pages;     /* pages in the pool                                            */
+  int32_t max_pages;   /* entries of a row's table                                     */
+  int32_t weighted;    /* 1: attention adds up what every token gets                   */
+} lq_config_paged;
+
+typedef struct {
+  void     *k_pages, *v_pages;
+  int32_t  *table;
+  float    *weights;     /* null unless `weighted`                                       */
+  int32_t  *n;           /* HOST [B]: tokens that row b holds                            */
+  int32_t  *cur;         /* HOST [B]: which half of table and weights is row b's         */
+  int32_t  *pages;       /* HOST [2][B]: entries of table that name pages                */
+  void     *seq_state;   /* DEVICE scratch, lq_sizes_paged.seq_state bytes               */
+} lq_cache_paged;
+
+/* Byte sizes (HOST out): pages is of one tensor (K or V). */
+typedef struct {
+  size_t pages, table, weights, seq_state;
+  size_t workspace;      /* of decode_attn, decode_step and evict                        */
+} lq_sizes_paged;
+lq_status logquant_sizes_paged(const lq_config_paged *cfg, lq_sizes_paged *out);
+
+/* Prepare a freshly allocated workspace (lq_sizes_paged.workspace bytes), as
+ * logquant_workspace_init does. */
+lq_status logquant_workspace_init_paged(const lq_config_paged *cfg, void *workspace, void *stream);
+
+/* New tokens behind those that each row holds; k_new, v_new, n_new, n_max as for
+ * logquant_append8.
+ *   rope      : null, or the keys are turned on their way (v_new is not);
+ *   positions : DEVICE [B][n_max] int32, with a rope; null: those behind the row's tokens,
+ *               n[b], n[b]+1, .. (the right ones until a row has been evicted from).
+ * New tokens of a weighted cache have weight 0.  LQ_ERR_CAPACITY if a row would pass its
+ * pages[cur[b]][b] pages.  On success n[b] += n_new[b]; the caller may set n[b] back to
+ * drop tokens. */
+lq_status logquant_append_paged(const lq_config_paged *cfg, lq_cache_paged *cache, const lq_rope *rope,
+                                const int32_t *positions, const void *k_new, const void *v_new,
+                                const int32_t *n_new, int32_t n_max, void *stream);
+
+/* How scores differ from scale * q . k (null: they do not).  In this order:
+ *   softcap > 0: s becomes softcap * tanh(s / softcap);
+ *   slopes (DEVICE, Hq floats, or null): s -= slopes[head] * (n-1 - t), t the token's place
+ *     in the row, n-1 the newest one's;
+ *   window > 0: tokens t < n - window get no weight.
+ * Distances are counted in tokens that the row holds; evicted ones do not count. */
+typedef struct {
+  float   softcap;
+  int32_t window;
+  const float *slopes;
+} lq_scores;
+
+/* Decode attention over the paged cache: out[b][h] = softmax_t(s_t) applied to v_t, t running
+ * over the tokens that row b holds; zeros for an empty row (or one without a page).
+ * Weighted: weights[b][h][t] += the sum, over the query heads of kv head h, of the
+ * probabilities of t.
+ * Finite scores within fp32.  q, out, softmax_scale, workspace: as for
+ * logquant_decode_attn8 (sizes from logquant_sizes_paged, prepared with
+ * logquant_workspace_init_paged).  LQ_ERR_SHAPE for a negative window, or a softcap or
+ * scale that is not finite or whose quotient is not. */
+lq_status logquant_decode_attn_paged(const lq_config_paged *cfg, lq_cache_paged *cache, const lq_scores *scores,
+                                     const void *q, float softmax_scale, void *out, void *workspace, void *stream);
+
+/* One decode step: q and the new key of every row turned by rope (null: not) at
+ * positions[b] (DEVICE [B]; null: n[b]), logquant_append_paged of that token, and
+ * logquant_decode_attn_paged with that query over the cache including it, with the results
+ * of the three calls (outputs and weights up to the order of fp32 sums).
+ *   k_new, v_new : DEVICE [B][Hkv][1][d] T.  LQ_ERR_CAPACITY if a row has no room. */
+lq_status logquant_decode_step_paged(const lq_config_paged *cfg, lq_cache_paged *cache, const lq_rope *rope,
+                                     const int32_t *positions, const lq_scores *scores, const void *k_new,
+                                     const void *v_new, const void *q, float softmax_scale, void *out,
+                                     void *workspace, void *stream);
+
+/* Eviction by accumulated attention (heavy hitters and recent tokens stay), of a
+ * weighted cache: of every row with n[b] > keep[b] (HOST [B]) each kv head keeps the newest
+ * `recent` tokens and the keep[b] - recent others with the largest weights, among equal
+ * ones those that came first.  They move, in order, to slots 0 .. keep[b]-1 of the pages
+ * that the other half of the table names for row b, their weights to the other half of
+ * weights, and that half becomes the row's: n[b] = keep[b], cur[b] flips.  The pages of the
+ * half that was are the caller's again.  Other rows stay as they are.
+ * Weights are compared as fp32 numbers and must not be NaN.  New pages must not be among
+ * those that a row reads.  LQ_ERR_STATE unless `weighted`; LQ_ERR_SHAPE for a negative keep,
+ * recent < 0, or recent > keep[b] of a row that loses tokens; LQ_ERR_CAPACITY if
+ * pages[1-cur[b]][b] are too few for keep[b] tokens. */
+lq_status logquant_evict_paged(const lq_config_paged *cfg, lq_cache_paged *cache, const int32_t *keep,
+                               int32_t recent, void *workspace, void *stream);
+
 /* Measurement helper (not a step of the method): one streaming read of `bytes` bytes of
  * DEVICE memory at `buf` (16-byte aligned, bytes >= 16; a tail of bytes % 16 is not read),
  * enqueued on `stream`.  `sink`: DEVICE, 8192 uint32 words the kernel folds what it read

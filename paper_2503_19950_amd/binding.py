@@ -63,6 +63,27 @@ class lq_sizes8(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("codes", "scale", "tail", "seq_state", "workspace")]
 
 
+class lq_rope(C.Structure):
+    _fields_ = [("dims", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float), ("freq", C.c_void_p)]
+
+
+class lq_scores(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p)]
+
+
+class lq_config_paged(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "page", "dtype", "n_pages", "max_pages", "weighted")]
+
+
+class lq_cache_paged(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "table", "weights")] + [
+        (n, C.POINTER(C.c_int32)) for n in ("n", "cur", "pages")] + [("seq_state", C.c_void_p)]
+
+
+class lq_sizes_paged(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("pages", "table", "weights", "seq_state", "workspace")]
+
+
 class lq_plan(C.Structure):
     _fields_ = [("blocks", C.c_int32), ("waves_per_block", C.c_int32), ("splits", C.c_int32),
                 ("fp_waves", C.c_int32), ("bytes_read", C.c_int64)]
@@ -75,6 +96,9 @@ EXPORTS = ("logquant_sizes", "logquant_workspace_bytes", "logquant_workspace_ini
            "logquant_decode_attn_seq", "logquant_decode_step_seq", "logquant_decode_plan_seq",
            "logquant_sizes8", "logquant_workspace_init8", "logquant_append8", "logquant_read8",
            "logquant_decode_attn8", "logquant_decode_step8",
+           "logquant_rope_frequencies", "logquant_rotate",
+           "logquant_sizes_paged", "logquant_workspace_init_paged", "logquant_append_paged", "logquant_decode_attn_paged",
+           "logquant_decode_step_paged", "logquant_evict_paged",
            "logquant_read_probe", "logquant_status_string")
 
 if not os.path.exists(LIB_PATH):
@@ -145,6 +169,25 @@ _lib.logquant_decode_attn8.restype = C.c_int
 _lib.logquant_decode_step8.argtypes = [C.POINTER(lq_config8), C.POINTER(lq_cache8), C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
 _lib.logquant_decode_step8.restype = C.c_int
+_ROPEP, _CFGP, _CACHEP = C.POINTER(lq_rope), C.POINTER(lq_config_paged), C.POINTER(lq_cache_paged)
+_lib.logquant_rope_frequencies.argtypes = [C.c_int32] + [C.c_double] * 5 + [C.POINTER(C.c_double)]
+_lib.logquant_rope_frequencies.restype = C.c_int
+_lib.logquant_rotate.argtypes = [_ROPEP] + [C.c_int32] * 6 + [C.c_void_p] * 6
+_lib.logquant_rotate.restype = C.c_int
+_lib.logquant_sizes_paged.argtypes = [_CFGP, C.POINTER(lq_sizes_paged)]
+_lib.logquant_sizes_paged.restype = C.c_int
+_lib.logquant_workspace_init_paged.argtypes = [_CFGP, C.c_void_p, C.c_void_p]
+_lib.logquant_workspace_init_paged.restype = C.c_int
+_lib.logquant_append_paged.argtypes = [_CFGP, _CACHEP, _ROPEP, C.c_void_p, C.c_void_p, C.c_void_p, _I32P, C.c_int32, C.c_void_p]
+_lib.logquant_append_paged.restype = C.c_int
+_lib.logquant_decode_attn_paged.argtypes = [_CFGP, _CACHEP, C.POINTER(lq_scores), C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
+                                            C.c_void_p]
+_lib.logquant_decode_attn_paged.restype = C.c_int
+_lib.logquant_decode_step_paged.argtypes = [_CFGP, _CACHEP, _ROPEP, C.c_void_p, C.POINTER(lq_scores), C.c_void_p, C.c_void_p,
+                                            C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.logquant_decode_step_paged.restype = C.c_int
+_lib.logquant_evict_paged.argtypes = [_CFGP, _CACHEP, _I32P, C.c_int32, C.c_void_p, C.c_void_p]
+_lib.logquant_evict_paged.restype = C.c_int
 _lib.logquant_read_probe.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
 _lib.logquant_read_probe.restype = C.c_int
 _lib.logquant_status_string.argtypes = [C.c_int]
@@ -310,6 +353,50 @@ def logquant_decode_step8(cfg, cache, k_new, v_new, q, softmax_scale, out, works
                                       _ptr(out), _ptr(workspace), stream)
 
 
+def logquant_rope_frequencies(dims, base=10000.0, stretch=1.0, original=0.0, slow=1.0, fast=32.0):
+    """-> list of dims/2 radians per position; host arithmetic only."""
+    freq = (C.c_double * max(1, dims // 2))()
+    st = _lib.logquant_rope_frequencies(int(dims), base, stretch, original, slow, fast, freq)
+    if st != LQ_OK:
+        raise LogQuantError(st, "logquant_rope_frequencies")
+    return list(freq)
+
+
+def logquant_rotate(rope, B, L, Hq, Hkv, d, dtype, positions, q, q_out, k, k_out, stream=0):
+    return _lib.logquant_rotate(_p(rope), B, L, Hq, Hkv, d, dtype, _ptr(positions), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), stream)
+
+
+def logquant_sizes_paged(cfg):
+    out = lq_sizes_paged()
+    st = _lib.logquant_sizes_paged(_p(cfg), C.byref(out))
+    if st != LQ_OK:
+        raise LogQuantError(st, "logquant_sizes_paged")
+    return out
+
+
+def logquant_workspace_init_paged(cfg, workspace, stream=0):
+    return _lib.logquant_workspace_init_paged(_p(cfg), _ptr(workspace), stream)
+
+
+def logquant_append_paged(cfg, cache, rope, positions, k_new, v_new, n_new, n_max, stream=0):
+    return _lib.logquant_append_paged(_p(cfg), _p(cache), _p(rope), _ptr(positions), _ptr(k_new), _ptr(v_new), _i32(n_new), int(n_max),
+                                      stream)
+
+
+def logquant_decode_attn_paged(cfg, cache, scores, q, softmax_scale, out, workspace, stream=0):
+    return _lib.logquant_decode_attn_paged(_p(cfg), _p(cache), _p(scores), _ptr(q), float(softmax_scale), _ptr(out), _ptr(workspace),
+                                           stream)
+
+
+def logquant_decode_step_paged(cfg, cache, rope, positions, scores, k_new, v_new, q, softmax_scale, out, workspace, stream=0):
+    return _lib.logquant_decode_step_paged(_p(cfg), _p(cache), _p(rope), _ptr(positions), _p(scores), _ptr(k_new), _ptr(v_new), _ptr(q),
+                                           float(softmax_scale), _ptr(out), _ptr(workspace), stream)
+
+
+def logquant_evict_paged(cfg, cache, keep, recent, workspace, stream=0):
+    return _lib.logquant_evict_paged(_p(cfg), _p(cache), _i32(keep), int(recent), _ptr(workspace), stream)
+
+
 def torch_dtype(dtype):
     import torch
     return torch.bfloat16 if dtype == "bf16" else torch.float16
@@ -329,6 +416,10 @@ def make_config(B, Hq, Hkv, d, fp_budget, group, dtype, q_capacity, bits=2):
 
 def make_config8(B, Hq, Hkv, d, block, dtype, capacity):
     return lq_config8(B, Hq, Hkv, d, block, LQ_BF16 if dtype == "bf16" else LQ_F16, capacity)
+
+
+def make_config_paged(B, Hq, Hkv, d, page, dtype, n_pages, max_pages, weighted=False):
+    return lq_config_paged(B, Hq, Hkv, d, page, LQ_BF16 if dtype == "bf16" else LQ_F16, n_pages, max_pages, int(weighted))
 
 
 class DeviceCache:
@@ -599,3 +690,240 @@ class DeviceCache8:
         self._call("logquant_decode_step8", self._c, self._address("k_new", k_new, self._token), self._address("v_new", v_new, self._token),
                    self._address("q", q, self._q_shape), softmax_scale, self._address("out", out, self._q_shape), self._ws)
         return out
+
+
+def _cuda(device):
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError("Expected a cuda device, but got: %s" % device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+
+
+def _tensor(name, t, shape, dtype, device):
+    """Address of a tensor that is what a call takes."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device.index or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
+    return t.data_ptr()
+
+
+def _on_device(index, name, *args):
+    """An entry point on the current stream of device `index`, whichever device is current."""
+    f = getattr(_lib, name)
+    if torch._C._cuda_getDevice() == index:
+        st = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    if st != LQ_OK:
+        raise LogQuantError(st, name)
+
+
+class Rope:
+    """Rotary positions: frequencies (radians per position of every pair, as logquant_rope_frequencies gives them) on a
+    device, which pairs they turn, and a factor on what is turned."""
+
+    def __init__(self, freq, interleaved=False, factor=1.0, device="cuda:0"):
+        self.device = _cuda(device)
+        self.freq = torch.as_tensor(freq, dtype=torch.float64).to(self.device).contiguous()
+        if self.freq.dim() != 1 or not len(self.freq):
+            raise ValueError("freq: expected one frequency for every pair")
+        self.c = lq_rope(2 * len(self.freq), int(interleaved), factor, self.freq.data_ptr())
+        self._c = C.byref(self.c)
+
+
+def rotate(rope, positions=None, q=None, k=None, q_out=None, k_out=None):
+    """q [B][Hq][L][d], or [B][Hq][d] for L = 1, and k [B][Hkv][L][d], either may be None, turned by positions ([B][L] int32,
+    or [B]; None: 0 .. L-1): into the given tensors, which may be q and k themselves, or new ones.  -> (q_out, k_out).
+    The call goes to the current stream of the rope's device."""
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("rotate: no tensor")
+    if x.dim() not in (3, 4) or x.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("rotate: expected fp16 or bf16 tensors of shape [B][H][L][d] or [B][H][d]")
+    B, L, d = x.shape[0], x.shape[2] if x.dim() == 4 else 1, x.shape[-1]
+    heads, at = [], []
+    for name, t, out in (("q", q, q_out), ("k", k, k_out)):
+        if t is None:
+            if out is not None:
+                raise ValueError("%s_out without %s" % (name, name))
+            heads.append(0)
+            at += [None, None]
+            continue
+        shape = torch.Size((B, t.shape[1] if t.dim() > 1 else 0, L, d) if t.dim() == 4 else (B, t.shape[1] if t.dim() > 1 else 0, d))
+        if L != 1 and t.dim() != 4:
+            raise ValueError("%s: expected [B][H][L][d]" % name)
+        src = _tensor(name, t, shape, x.dtype, rope.device)
+        if out is None:
+            out = torch.empty_like(t)
+        dst = _tensor(name + "_out", out, shape, x.dtype, rope.device)
+        heads.append(shape[1])
+        at += [src, dst]
+        if name == "q":
+            q_out = out
+        else:
+            k_out = out
+    p = None
+    if positions is not None:
+        p = _tensor("positions", positions, torch.Size((B,) if positions.dim() == 1 and L == 1 else (B, L)), torch.int32, rope.device)
+    _on_device(rope.device.index, "logquant_rotate", rope._c, B, L, heads[0], heads[1], d, LQ_BF16 if x.dtype is torch.bfloat16 else LQ_F16,
+               p, *at)
+    return q_out, k_out
+
+
+class DeviceCachePaged:
+    """Owner of the device buffers of one lq_cache_paged (torch tensors), its counts, tables and workspace, and of the pool's
+    free pages.  Tensors are refused (ValueError) unless they are of the cache's type, shape and device and contiguous.  A call
+    goes to the current stream of the cache's device, whichever device is current."""
+
+    BUFFERS = ("k_pages", "v_pages", "table", "weights")
+
+    def __init__(self, cfg, device="cuda:0", poison=False):
+        self.cfg = cfg
+        self.device = _cuda(device)
+        self.dtype = torch_dtype("bf16" if cfg.dtype == LQ_BF16 else "f16")
+        self.sizes = logquant_sizes_paged(cfg)
+        B = cfg.B
+
+        def buf(nbytes):
+            return torch.full((int(nbytes),), 0xFF if poison else 0, dtype=torch.uint8, device=self.device)
+
+        self.k_pages, self.v_pages = buf(self.sizes.pages), buf(self.sizes.pages)
+        self.table = torch.full((2, B, cfg.max_pages), -1, dtype=torch.int32, device=self.device)
+        self.weights = buf(self.sizes.weights).view(torch.float32).view(2, B, cfg.Hkv, -1) if cfg.weighted else None
+        self.seq_state, self.workspace = buf(self.sizes.seq_state), buf(self.sizes.workspace)
+        self.n, self.cur, self.pages = (C.c_int32 * B)(), (C.c_int32 * B)(), (C.c_int32 * (2 * B))()
+        self.ids = [[[] for _ in range(B)] for _ in range(2)]     # pages that the table names, by half and row
+        self.free = list(range(cfg.n_pages - 1, -1, -1))
+        self.c = lq_cache_paged(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.table.data_ptr(),
+                                self.weights.data_ptr() if cfg.weighted else None, *(C.cast(x, _I32P) for x in (self.n, self.cur, self.pages)),
+                                self.seq_state.data_ptr())
+        # what every call takes, made once
+        self._index = self.device.index
+        self._cfg, self._c, self._ws = C.byref(cfg), C.byref(self.c), self.workspace.data_ptr()
+        self._q_shape, self._token = torch.Size((B, cfg.Hq, cfg.d)), torch.Size((B, cfg.Hkv, 1, cfg.d))
+        self._scores, self._scores_of = None, (0.0, 0, None)
+        _on_device(self._index, "logquant_workspace_init_paged", self._cfg, self._ws)
+
+    # ---- pages
+    def set_pages(self, b, ids, spare=False):
+        """The pages of row b's tokens, in order (`spare`: those that its next eviction moves to).  Pages that were named
+        there before and by no other row go back to the pool, pages named here leave it."""
+        ids = [int(i) for i in ids]
+        if len(ids) > self.cfg.max_pages or any(not 0 <= i < self.cfg.n_pages for i in ids):
+            raise ValueError("set_pages: expected up to %d pages in 0 .. %d" % (self.cfg.max_pages, self.cfg.n_pages - 1))
+        if not spare and len(ids) * self.cfg.page < self.n[b]:
+            raise ValueError("set_pages: row %d holds %d tokens" % (b, self.n[b]))
+        half = self.cur[b] ^ int(bool(spare))
+        before, self.ids[half][b] = self.ids[half][b], ids
+        used = {i for part in self.ids for row in part for i in row}
+        known = set(self.free)
+        self.free = [i for i in self.free if i not in used] + [i for i in dict.fromkeys(before) if i not in used and i not in known]
+        self._name(half, b, 0)
+
+    def _name(self, half, b, first):
+        ids = self.ids[half][b]
+        if len(ids) > first:
+            self.table[half, b, first:len(ids)] = torch.tensor(ids[first:], dtype=torch.int32)
+        self.pages[half * self.cfg.B + b] = len(ids)
+
+    def reserve(self, counts, spare=False):
+        """Pages out of the pool for counts[b] tokens of every row (`spare`: for its next eviction).  LogQuantError
+        (LQ_ERR_CAPACITY) if the pool or a row's table has too few; nothing is taken then."""
+        cfg = self.cfg
+        if len(counts) != cfg.B:
+            raise ValueError("reserve: expected %d counts" % cfg.B)
+        more = []
+        for b, count in enumerate(counts):
+            half = self.cur[b] ^ int(bool(spare))
+            need = -(-int(count) // cfg.page) - len(self.ids[half][b])
+            if need > 0:
+                more.append((half, b, need))
+            if len(self.ids[half][b]) + max(need, 0) > cfg.max_pages:
+                raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
+        if sum(need for _, _, need in more) > len(self.free):
+            raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
+        for half, b, need in more:
+            first = len(self.ids[half][b])
+            self.ids[half][b] += [self.free.pop() for _ in range(need)]
+            self._name(half, b, first)
+
+    def release(self, b, spare=False):
+        """Row b gives its pages back and is empty (`spare`: gives back those that it has for its next eviction, or had
+        before its last)."""
+        if not spare:
+            self.n[b] = 0
+        self.set_pages(b, [], spare)
+
+    # ---- counts
+    def counts(self):
+        return list(self.n)
+
+    def set_counts(self, counts, cur=None):
+        """Set the host-side counts (the device buffers are left as they are), and, where given, which half is every row's."""
+        self.n[:] = counts
+        if cur is not None:
+            self.cur[:] = cur
+
+    # ---- calls
+    def _turn(self, rope, positions, n):
+        if rope is None:
+            if positions is not None:
+                raise ValueError("positions without a rope")
+            return None, None
+        if rope.device != self.device:
+            raise ValueError("rope: expected it on %s" % self.device)
+        if positions is None:
+            return rope._c, None
+        shape = torch.Size((self.cfg.B,) if n == 1 and positions.dim() == 1 else (self.cfg.B, n))
+        return rope._c, _tensor("positions", positions, shape, torch.int32, self.device)
+
+    def _how(self, softcap, window, slopes):
+        if not softcap and not window and slopes is None:
+            return None
+        at = None if slopes is None else _tensor("slopes", slopes, torch.Size((self.cfg.Hq,)), torch.float32, self.device)
+        if (softcap, window, at) != self._scores_of or self._scores is None:
+            self._scores, self._scores_of = lq_scores(softcap, window, at), (softcap, window, at)
+        return C.byref(self._scores)
+
+    def append(self, k_new, v_new, n_new=None, rope=None, positions=None):
+        """k_new, v_new: [B][Hkv][n][d]; n_new: tokens that each row takes of them, 0..n (None: all).  With a rope, keys are
+        turned by positions ([B][n] int32; None: the places of the tokens)."""
+        c = self.cfg
+        n = k_new.shape[2] if k_new.dim() == 4 else 1
+        shape = self._token if n == 1 else torch.Size((c.B, c.Hkv, n, c.d))
+        k, v = _tensor("k_new", k_new, shape, self.dtype, self.device), _tensor("v_new", v_new, shape, self.dtype, self.device)
+        if n_new is not None and len(n_new) != c.B:
+            raise ValueError("n_new: expected %d counts" % c.B)
+        turn, at = self._turn(rope, positions, n)
+        _on_device(self._index, "logquant_append_paged", self._cfg, self._c, turn, at, k, v, _i32(n_new), n)
+
+    def decode_attn(self, q, out=None, softmax_scale=0.0, softcap=0.0, window=0, slopes=None):
+        """q: [B][Hq][d]; rows of the batch that hold no token give zeros.  slopes: [Hq] fp32."""
+        if out is None:
+            out = torch.empty_like(q)
+        _on_device(self._index, "logquant_decode_attn_paged", self._cfg, self._c, self._how(softcap, window, slopes),
+                   _tensor("q", q, self._q_shape, self.dtype, self.device), softmax_scale,
+                   _tensor("out", out, self._q_shape, self.dtype, self.device), self._ws)
+        return out
+
+    def decode_step(self, k_new, v_new, q, out=None, softmax_scale=0.0, rope=None, positions=None, softcap=0.0, window=0, slopes=None):
+        """Append one token per row ([B][Hkv][1][d]) and attend; with a rope, its key and the query are turned by positions
+        ([B] int32; None: the places of the tokens)."""
+        if out is None:
+            out = torch.empty_like(q)
+        turn, at = self._turn(rope, positions, 1)
+        _on_device(self._index, "logquant_decode_step_paged", self._cfg, self._c, turn, at, self._how(softcap, window, slopes),
+                   _tensor("k_new", k_new, self._token, self.dtype, self.device), _tensor("v_new", v_new, self._token, self.dtype, self.device),
+                   _tensor("q", q, self._q_shape, self.dtype, self.device), softmax_scale,
+                   _tensor("out", out, self._q_shape, self.dtype, self.device), self._ws)
+        return out
+
+    def evict(self, keep, recent=0):
+        """Rows with more than `keep` tokens (a number, or one for every row) keep the newest `recent` and the heaviest
+        others, in pages that are taken from the pool if the row has too few spare ones.  The pages that it leaves are its
+        spare ones (`release(b, spare=True)` gives them back)."""
+        keep = [int(keep)] * self.cfg.B if isinstance(keep, int) else [int(x) for x in keep]
+        if len(keep) != self.cfg.B:
+            raise ValueError("keep: expected %d counts" % self.cfg.B)
+        self.reserve([x if n > x else 0 for n, x in zip(self.n, keep)], spare=True)
+        _on_device(self._index, "logquant_evict_paged", self._cfg, self._c, _i32(keep), recent, self._ws)

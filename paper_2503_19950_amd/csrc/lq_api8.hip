@@ -1,7 +1,5 @@
 // C ABI of the 8-bit cache: argument checks on the host, then kernel launches.
 #include <math.h>
-#include <stdlib.h>
-
 
 #include "lq_cache8.h"
 #include "lq_internal.h"
@@ -28,8 +26,6 @@ static lq_status make_shape8(const lq_config8* cfg, Shape8* s) {
   return LQ_OK;
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
 // Common start of the calls: shape, pointers, counts.
 static lq_status begin8(const lq_config8* cfg, const lq_cache8* c, Shape8* s) {
   const lq_status st = make_shape8(cfg, s);
@@ -43,32 +39,12 @@ static lq_status begin8(const lq_config8* cfg, const lq_cache8* c, Shape8* s) {
   return LQ_OK;
 }
 
-// One entry for each batch row: on the stack for the batches that travel in a launch's arguments, else from the heap.
-struct RowList {
-  Row8 few[ROWS_IN_ARGS];
-  Row8* many = nullptr;
-  Row8* e;
-  int n;
-  explicit RowList(int rows) : e(few), n(rows) {
-    if (n > ROWS_IN_ARGS) e = many = static_cast<Row8*>(malloc(n * sizeof(Row8)));
-  }
-  ~RowList() { free(many); }
-  RowList(const RowList&) = delete;
-  bool ok() const { return e != nullptr; }
-  bool alike() const {
-    for (int b = 1; b < n; ++b)
-      if (e[b].n != e[0].n || e[b].x != e[0].x) return false;
-    return true;
-  }
-  RowArg8 arg(const lq_cache8* c, bool same) const { return RowArg8{e, (Row8*)c->seq_state, n, same}; }
-};
-
 static lq_status attend8(const Shape8& s, const lq_cache8& c, RowList* rows, const void* k_new, const void* v_new, const void* q,
                          float softmax_scale, void* out, void* workspace, hipStream_t stream) {
   Plan8 plan;
   const bool same = plan8(s, rows->alike(), k_new != nullptr, rows->e, rows->n, &plan);
   if (!(softmax_scale > 0.f)) softmax_scale = 1.0f / sqrtf((float)s.d);
-  return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, rows->arg(&c, same), stream) == hipSuccess ? LQ_OK
+  return launch_attn8(s, c, q, softmax_scale, out, workspace, plan, k_new, v_new, rows->arg(c.seq_state, same), stream) == hipSuccess ? LQ_OK
                                                                                                                              : LQ_ERR_HIP;
 }
 
@@ -121,7 +97,7 @@ lq_status logquant_append8(const lq_config8* cfg, lq_cache8* cache, const void* 
   }
   if (!blocks) return LQ_OK;   // nobody takes a token
   clear_stale_error();
-  if (launch_append8(s, *cache, k_new, v_new, n_max, blocks, rows.arg(cache, rows.alike()), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
+  if (launch_append8(s, *cache, k_new, v_new, n_max, blocks, rows.arg(cache->seq_state, rows.alike()), (hipStream_t)stream) != hipSuccess) return LQ_ERR_HIP;
   for (int b = 0; b < s.B; ++b) cache->n[b] += rows.e[b].x;
   return LQ_OK;
 }
@@ -141,7 +117,7 @@ lq_status logquant_read8(const lq_config8* cfg, const lq_cache8* cache, int32_t 
   }
   if (longest <= t0) return LQ_OK;   // nothing of the range is there
   clear_stale_error();
-  return launch_read8(s, *cache, t0, n, k_out, v_out, rows.arg(cache, rows.alike()), (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_HIP;
+  return launch_read8(s, *cache, t0, n, k_out, v_out, rows.arg(cache->seq_state, rows.alike()), (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_HIP;
 }
 
 lq_status logquant_decode_attn8(const lq_config8* cfg, const lq_cache8* cache, const void* q, float softmax_scale, void* out,

@@ -1,0 +1,183 @@
+// The paged cache: writing tokens.
+//
+// Bound by the bytes.  A workgroup takes a unit of 32 slots of a row and some kv heads, a head a wavefront; with rotary
+// positions it computes the unit's cosines and sines once, into LDS.  Keys go over 16 bytes a lane, as they lie in a row of
+// the prompt; values as two channels of eight tokens a lane, whose halves are the pieces of the page.
+#include "lq_internal.h"
+#include "lq_paged.h"
+#include "lq_quant8.h"
+
+namespace lq {
+
+namespace {
+
+constexpr int WAVES = 4, PITCH = 66;         // pairs from one token's angles to the next (64 and padding)
+
+struct AppendPagedParams {
+  const uint16_t *k_new, *v_new;
+  uint16_t *k_pages, *v_pages;
+  const int* table;
+  float* weights;                            // null unless the cache keeps them
+  RopeArg rope;
+  const Row8* rows;
+  Row8 same;
+  int B, Hkv, heads, log_p, n_pages, max_pages, n_max;       // heads: of a workgroup
+};
+
+__device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0); }
+__device__ __forceinline__ uint16_t load2(__amdgpu_buffer_rsrc_t rs, int off) { return __builtin_amdgcn_raw_buffer_load_b16(rs, off, 0, 0); }
+// token within its unit of 32 at position e of the eight that lane row a holds
+__device__ __forceinline__ int value_token(int a, int e) { return 16 * (e >> 2) + 4 * a + (e & 3); }
+
+// Channels c0 .. c0+7 of a key (offset `row` of rs), turned; angle: that token's.
+template <bool BF16>
+__device__ __forceinline__ u32x4 turned(__amdgpu_buffer_rsrc_t rs, int row, int c0, u32x4 x, const RopeArg& rope, const float2* angle) {
+  const int dims = rope.dims, half = dims / 2;
+  if (rope.interleaved) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (c0 + 2 * w >= dims) break;
+      uint16_t p = (uint16_t)x[w], o = (uint16_t)(x[w] >> 16);
+      turn_pair<BF16>(p, o, angle[c0 / 2 + w]);
+      x[w] = p | (uint32_t)o << 16;
+    }
+    return x;
+  }
+  if (c0 >= dims) return x;
+  u32x4 y{0, 0, 0, 0};                       // the pairs' other halves
+  if (dims % 16 == 0) {
+    y = load16(rs, row + 2 * (c0 < half ? c0 + half : c0 - half));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = c0 + e;
+      if (c < dims) y[e / 2] |= (uint32_t)load2(rs, row + 2 * (c < half ? c + half : c - half)) << (16 * (e & 1));
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int c = c0 + e, sh = 16 * (e & 1);
+    if (c >= dims) break;
+    const bool first = c < half;
+    uint16_t own = (uint16_t)(x[e / 2] >> sh), other = (uint16_t)(y[e / 2] >> sh);
+    const float2 cs = angle[first ? c : c - half];
+    uint16_t p = first ? own : other, o = first ? other : own;
+    turn_pair<BF16>(p, o, cs);
+    x[e / 2] = (x[e / 2] & ~(0xFFFFu << sh)) | (uint32_t)(first ? p : o) << sh;
+  }
+  return x;
+}
+
+// grid (units that a row's new tokens touch, shares of the kv heads, B)
+template <bool BF16, int D, int MODE, bool TURN>
+__global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPagedParams P, const Rows8<MODE> S) {
+  (void)S;
+  constexpr int ND = D / 32;
+  const int b = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane / 16;
+  Row8 row = P.same;
+  if constexpr (MODE == ROWS_LISTED) {
+    const Row8Ptr r = rows_ptr(P.rows, sizeof(AppendPagedParams));
+    row = Row8{r[b].n, r[b].x, 1, r[b].b};
+  } else {
+    row.b += b;
+  }
+  const int unit = row.n / 32 + (int)blockIdx.x, end = row.n + row.x;
+  if (32 * unit >= end || row.x == 0) return;
+  const int low = row.n > 32 * unit ? row.n - 32 * unit : 0, high = end - 32 * unit < 32 ? end - 32 * unit : 32;
+  const int head0 = blockIdx.y * P.heads, head1 = head0 + P.heads < P.Hkv ? head0 + P.heads : P.Hkv;
+  const int64_t new0 = 32 * (int64_t)unit + low - row.n;                // token `low` of the unit among the new ones
+  if (P.weights)
+    for (int x = threadIdx.x; x < 32 * (head1 - head0); x += 64 * WAVES)
+      if (x % 32 >= low && x % 32 < high)
+        P.weights[((((int64_t)row.b * P.Hkv + head0 + x / 32) * P.max_pages) << P.log_p) + 32 * unit + x % 32] = 0.f;
+  const int id = P.table[(int64_t)row.b * P.max_pages + (unit >> (P.log_p - 5))];
+  if (!is_page(id, P.n_pages)) return;
+  __shared__ __align__(16) float2 cs[TURN ? 32 * PITCH : 1];
+  if constexpr (TURN) {
+    const int pairs = P.rope.dims / 2;
+    for (int x = threadIdx.x; x < (high - low) * pairs; x += 64 * WAVES) {
+      const int t = x / pairs, i = x - t * pairs;
+      const int position = P.rope.positions ? P.rope.positions[(int64_t)b * P.n_max + new0 + t] : 32 * unit + low + t;
+      cs[(low + t) * PITCH + i] = turn_of(P.rope.freq[i], position, P.rope.factor);
+    }
+    __syncthreads();
+  }
+  for (int h = head0 + wave; h < head1; h += WAVES) {
+    const int64_t from = (((int64_t)b * P.Hkv + h) * P.n_max + new0) * D;
+    // tokens outside low .. high - 1: zeros, not read
+    const __amdgpu_buffer_rsrc_t rk = buffer(P.k_new + from, (high - low) * D * 2), rv = buffer(P.v_new + from, (high - low) * D * 2);
+    const int64_t off = unit_offset(id, P.Hkv, h, P.log_p, unit, D);
+    u32x4 k[2 * ND];
+    uint32_t v[ND][8];
+#pragma unroll
+    for (int x = 0; x < 2 * ND; ++x) k[x] = load16(rk, (16 * (x / ND) + lane % 16 - low) * (2 * D) + 2 * (32 * (x % ND) + 8 * a));
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[nd][e] = load4(rv, (value_token(a, e) - low) * (2 * D) + 2 * (32 * nd + 2 * (lane % 16)));
+#pragma unroll
+    for (int x = 0; x < 2 * ND; ++x) {
+      const int t = 16 * (x / ND) + lane % 16, c = 32 * (x % ND) + 8 * a;
+      if (t < low || t >= high) continue;
+      u32x4 y = k[x];
+      if constexpr (TURN) y = turned<BF16>(rk, (t - low) * (2 * D), c, y, P.rope, cs + t * PITCH);
+      *reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8) = y;
+    }
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd) {
+      const int t0 = 4 * a, c = 32 * nd + 2 * (lane % 16);              // tokens t0 .. t0 + 3, t0 + 16 .. t0 + 19
+      if (t0 >= high || t0 + 19 < low) continue;
+      uint16_t* to = P.v_pages + off + v_fp_index(t0, c, 2 * ND);      // those of c, and behind them of c + 1
+      if (t0 >= low && t0 + 19 < high) {
+        auto piece = [&](uint32_t sel) {
+          return u32x4{__builtin_amdgcn_perm(v[nd][1], v[nd][0], sel), __builtin_amdgcn_perm(v[nd][3], v[nd][2], sel),
+                       __builtin_amdgcn_perm(v[nd][5], v[nd][4], sel), __builtin_amdgcn_perm(v[nd][7], v[nd][6], sel)};
+        };
+        reinterpret_cast<u32x4*>(to)[0] = piece(0x05040100);
+        reinterpret_cast<u32x4*>(to)[1] = piece(0x07060302);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = t0 + value_token(0, e);
+          if (t < low || t >= high) continue;
+          to[e] = (uint16_t)v[nd][e];
+          to[e + 8] = (uint16_t)(v[nd][e] >> 16);
+        }
+      }
+    }
+  }
+}
+
+template <int MODE>
+hipError_t append_paged(const ShapePaged& s, const AppendPagedParams& p, const Rows8<MODE>& rows, dim3 grid, hipStream_t st) {
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * WAVES), 0, st, p, rows); };
+  auto with = [&](auto t, auto turn) {
+    constexpr bool T = decltype(t)::value, TURN = decltype(turn)::value;
+    if (s.d == 64) return go(append_paged_kernel<T, 64, MODE, TURN>);
+    if (s.d == 96) return go(append_paged_kernel<T, 96, MODE, TURN>);
+    go(append_paged_kernel<T, 128, MODE, TURN>);
+  };
+  if (!p.rope.freq) with(std::false_type{}, std::false_type{});        // (the type does not matter)
+  else if (s.bf16) with(std::true_type{}, std::true_type{});
+  else with(std::false_type{}, std::true_type{});
+  return launch_status("append_paged");
+}
+
+}  // namespace
+
+hipError_t launch_append_paged(const ShapePaged& s, const lq_cache_paged& c, const RopeArg& rope, const void* k_new, const void* v_new,
+                               int n_max, int units, const RowArg8& rows, hipStream_t st) {
+  // heads of a workgroup share its angles; fewer where there are few workgroups
+  int heads = s.Hkv;
+  while (heads > WAVES && (int64_t)units * s.B * ((s.Hkv + heads - 1) / heads) < 1024) heads = (heads + 1) / 2;
+  AppendPagedParams p{(const uint16_t*)k_new, (const uint16_t*)v_new, (uint16_t*)c.k_pages, (uint16_t*)c.v_pages, c.table,
+                      s.weighted ? c.weights : nullptr, rope, nullptr, rows.host[0], s.B, s.Hkv, heads, log2_of(s.P), s.n_pages, s.max_pages,
+                      n_max};
+  const dim3 grid(units, (s.Hkv + heads - 1) / heads, s.B);
+  if (rows.same) return append_paged<ROWS_SAME>(s, p, Rows8<ROWS_SAME>{}, grid, st);
+  Rows8<ROWS_LISTED> listed{};
+  const hipError_t e = hand_over(rows, &listed, &p.rows, st);
+  return e != hipSuccess ? e : append_paged<ROWS_LISTED>(s, p, listed, grid, st);
+}
+
+}  // namespace lq

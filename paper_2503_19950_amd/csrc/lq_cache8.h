@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <stdlib.h>
 
 #include "../../include/logquant.h"
 #include "lq_deal8.h"
@@ -17,6 +18,28 @@ struct RowArg8 {
   int n;
   bool same;
 };
+// One entry for each batch row: on the stack for the batches that travel in a launch's arguments, else from the heap.
+struct RowList {
+  Row8 few[ROWS_IN_ARGS];
+  Row8* many = nullptr;
+  Row8* e;
+  int n;
+  explicit RowList(int rows) : e(few), n(rows) {
+    if (n > ROWS_IN_ARGS) e = many = static_cast<Row8*>(malloc(n * sizeof(Row8)));
+  }
+  ~RowList() { free(many); }
+  RowList(const RowList&) = delete;
+  bool ok() const { return e != nullptr; }
+  bool alike() const {
+    for (int b = 1; b < n; ++b)
+      if (e[b].n != e[0].n || e[b].x != e[0].x) return false;
+    return true;
+  }
+  RowArg8 arg(void* seq_state, bool same) const { return RowArg8{e, (Row8*)seq_state, n, same}; }
+};
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
 enum RowMode { ROWS_SAME, ROWS_LISTED };
 template <int MODE> struct Rows8 {};                               // a kernel's last argument
 template <> struct Rows8<ROWS_LISTED> { Row8 e[ROWS_IN_ARGS]; };

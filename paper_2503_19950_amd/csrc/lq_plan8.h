@@ -69,14 +69,10 @@ inline int64_t largest_load(const Row8* r, int rows, int per_row, int most, int 
 //    64 of up to 1000 (512, 17) 16.7, 17.2, 17.6.  Near 24 units many items would do better with fewer wavefronts (100 rows of up to
 //    2000, 800 items, 32 units: 43.8, 40.8, 45.3; 200 x 4 kv heads 46.4, 44.7, 48.8; 100 of up to 1500 33.8, 32.4, 37.2), as do
 //    more than 1024, which balance by their number (200 of up to 2000: 75.6 with 4, 84.6 with 16).
-inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows, Plan8* p) {
+// The rows' work is in their x; `bytes`: what the launch reads, `lds`: bytes of LDS that its workgroups may ask for.
+inline bool plan_work8(const Shape8& s, int64_t bytes, int lds, bool same, Row8* rows, int n_rows, Plan8* p) {
   constexpr int CUS = 256, LEAST = 4;
-  int64_t tokens = 0;
-  for (int b = 0; b < n_rows; ++b) {
-    tokens += rows[b].n;
-    rows[b].x = units8(rows[b].n, s.G, step);          // until the end
-  }
-  p->groups = head_groups8(s, tokens * s.Hkv * s.d * 2 >= 24000000);
+  p->groups = head_groups8(s, bytes >= 24000000);
   p->hb = (s.gh + p->groups - 1) / p->groups;
   p->waves = 4;
   const int per_row = s.Hkv * p->groups;
@@ -133,13 +129,23 @@ inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows,
     // (by work, not by tokens: what is split has to come first)
     std::sort(first, last, [](const Row8& x, const Row8& y) { return x.x > y.x; });
   }
-  while (lds_bytes8(p->waves, p->hb, s.d) > 65536 || (p->hb > 16 && p->waves > 4)) p->waves /= 2;   // (LDS that a launch may ask for)
+  while (lds_bytes8(p->waves, p->hb, s.d) > lds || (p->hb > 16 && p->waves > 4)) p->waves /= 2;   // (LDS that a launch may ask for)
   p->blocks = 0;
   for (Row8* r = first; r != last; ++r) {
     r->x = p->blocks;
     p->blocks += r->parts * per_row;
   }
   return same;
+}
+
+// Of the 8-bit cache: units of 32 tokens, as codes 1 and in the tail 2 each.
+inline bool plan8(const Shape8& s, bool same, bool step, Row8* rows, int n_rows, Plan8* p) {
+  int64_t tokens = 0;
+  for (int b = 0; b < n_rows; ++b) {
+    tokens += rows[b].n;
+    rows[b].x = units8(rows[b].n, s.G, step);          // until the end
+  }
+  return plan_work8(s, tokens * s.Hkv * s.d * 2, 65536, same, rows, n_rows, p);
 }
 
 }  // namespace lq

@@ -1,0 +1,169 @@
+"""The paged cache on the GPU: what is written where, bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_19950_amd import binding
+from tests import gpu_util_paged as U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d,page", [(64, 32), (96, 64), (128, 128), (128, 32)])
+def test_append_in_pieces(d, page, dtype):
+    B, Hkv = 3, 2
+    cache = U.make(B, 4, Hkv, d, page, dtype, 12, seed=d)
+    model, before = U.Model(cache, dtype), U.pools(cache)
+    cache.reserve([12 * page - 1] * B)
+    for i, (n, n_new) in enumerate([(1, None), (40, [40, 0, 31]), (2 * page, [page, 2 * page, 1]), (3, [0, 3, 0]), (1, [1, 1, 0]), (33, None),
+                                    (page, None), (32, [32, 1, 31])]):
+        K, V = U.rows(10 + i, B, Hkv, n, d, dtype=dtype), U.rows(50 + i, B, Hkv, n, d, dtype=dtype)
+        cache.append(K.to(U.DEVICE), V.to(U.DEVICE), n_new)
+        model.append(K, V, n_new)
+        U.check_rows(cache, model, before)
+
+
+@pytest.mark.parametrize("dims,interleaved", [(128, False), (64, True), (48, False), (10, False), (10, True), (126, False)])
+def test_keys_turned_on_their_way_are_keys_turned_before(dims, interleaved):
+    B, Hkv, d, page, dtype = 2, 3, 128, 64, "bf16"
+    cache = U.make(B, 3, Hkv, d, page, dtype, 3)
+    model, before = U.Model(cache, dtype), U.pools(cache)
+    cache.reserve([150, 150])
+    rope = binding.Rope(binding.logquant_rope_frequencies(dims), interleaved, 0.75, U.DEVICE)
+    for i, n in enumerate([70, 1, 3]):
+        K, V = U.rows(i, B, Hkv, n, d, dtype=dtype), U.rows(9 + i, B, Hkv, n, d, dtype=dtype)
+        at = torch.randint(-100, 1 << 20, (B, n), generator=torch.Generator().manual_seed(i), dtype=torch.int32).to(U.DEVICE)
+        places = torch.tensor([[cache.n[b] + t for t in range(n)] for b in range(B)], dtype=torch.int32, device=U.DEVICE)
+        n_new = [n, max(0, n - 2)]
+        turned = binding.rotate(rope, at if i else places, k=K.to(U.DEVICE))[1].cpu()
+        cache.append(K.to(U.DEVICE), V.to(U.DEVICE), n_new, rope=rope, positions=at if i else None)
+        model.append(turned, V, n_new)
+        U.check_rows(cache, model, before)
+
+
+def test_more_rows_than_travel_with_a_launch():
+    B, d, dtype = 300, 64, "f16"
+    cache = U.make(B, 1, 1, d, 32, dtype, 2)
+    model, before = U.Model(cache, dtype), U.pools(cache)
+    cache.reserve([40] * B)
+    for n in (37, 1):
+        n_new = [b * 7 % (n + 1) for b in range(B)]
+        K, V = U.rows(n, B, 1, n, d, dtype=dtype), U.rows(n + 1, B, 1, n, d, dtype=dtype)
+        cache.append(K.to(U.DEVICE), V.to(U.DEVICE), n_new)
+        model.append(K, V, n_new)
+    U.check_rows(cache, model, before)
+
+
+def test_entries_that_are_no_pages_store_nothing():
+    B, Hkv, d, page, dtype = 2, 1, 64, 32, "f16"
+    cache = U.make(B, 1, Hkv, d, page, dtype, 4)
+    cache.reserve([128, 128])
+    model, before = U.Model(cache, dtype), U.pools(cache)
+    good = list(cache.ids[0][1])
+    cache.table[0, 1, 1] = -1
+    cache.table[0, 1, 2] = cache.cfg.n_pages
+    cache.table[0, 1, 3] = 2 ** 31 - 1
+    K, V = U.rows(1, B, Hkv, 128, d, dtype=dtype), U.rows(2, B, Hkv, 128, d, dtype=dtype)
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE))
+    model.append(K, V)
+    now = U.pools(cache)
+    for w, x in (("k", K), ("v", V)):
+        want = before[w].copy()
+        for b, n in ((0, 128), (1, 32)):
+            want[U.addresses(cache, w, b, 0, n)] = x[b, 0, :n].view(torch.int16).numpy()
+        assert np.array_equal(now[w], want)
+    q = U.rows(3, B, 1, d, dtype=dtype)
+    out = cache.decode_attn(q.to(U.DEVICE))
+    model.K[1], model.V[1] = model.K[1][:, :32], model.V[1][:, :32]      # row 1: its one page
+    model.check_output(out, q)
+    cache.table[0, 1] = -7                                               # no page at all
+    out = cache.decode_attn(q.to(U.DEVICE))
+    assert (out[1] == 0).all() and len(good) == 4
+    model.check_output(out, q, skip=(1,))
+
+
+def test_rows_that_share_a_prefix():
+    B, Hkv, d, page, dtype = 3, 2, 96, 32, "bf16"
+    cache = U.make(B, 4, Hkv, d, page, dtype, 4, n_pages=12)
+    K, V = U.rows(1, B, Hkv, 64, d, dtype=dtype), U.rows(2, B, Hkv, 64, d, dtype=dtype)
+    K[:], V[:] = K[:1], V[:1]
+    cache.reserve([64, 0, 0])
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), [64, 0, 0])
+    common = list(cache.ids[0][0])
+    for b in (1, 2):
+        cache.set_pages(b, common)
+        cache.n[b] = 64
+    model = U.Model(cache, dtype)
+    model.append(K, V)
+    cache.reserve([65, 70, 96])
+    before = U.pools(cache)
+    K, V = U.rows(3, B, Hkv, 32, d, dtype=dtype), U.rows(4, B, Hkv, 32, d, dtype=dtype)
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), [1, 6, 32])
+    model.append(K, V, [1, 6, 32])
+    U.check_rows(cache, model, before)
+    q = U.rows(5, B, 4, d, dtype=dtype)
+    model.check_output(cache.decode_attn(q.to(U.DEVICE)), q)
+    cache.release(0)
+    assert not set(common) & set(cache.free) and len(cache.free) == 12 - 2 - 2
+    cache.release(1)
+    cache.release(2)
+    assert sorted(cache.free) == list(range(12)) and cache.counts() == [0, 0, 0]
+
+
+def test_the_pool_runs_out():
+    cache = U.make(2, 1, 1, 64, 32, "f16", 8, n_pages=5)
+    cache.reserve([64, 33])
+    with pytest.raises(binding.LogQuantError):
+        cache.reserve([96, 65])
+    with pytest.raises(binding.LogQuantError):
+        cache.reserve([64, 257])
+    assert len(cache.free) == 1 and [len(x) for x in cache.ids[0]] == [2, 2]
+    with pytest.raises(ValueError):
+        cache.set_pages(0, [5])
+    with pytest.raises(ValueError):
+        cache.set_pages(0, [-1])
+    x = torch.zeros((2, 1, 65, 64), dtype=torch.float16, device=U.DEVICE)
+    with pytest.raises(binding.LogQuantError) as e:
+        cache.append(x, x)
+    assert e.value.status == binding.LQ_ERR_CAPACITY and cache.counts() == [0, 0]
+    cache.append(x[:, :, :64].contiguous(), x[:, :, :64].contiguous())
+    with pytest.raises(ValueError):
+        cache.set_pages(0, [1])
+
+
+def test_tensors_that_are_refused():
+    cache = U.make(2, 4, 2, 64, 32, "f16", 2, weighted=True)
+    cache.reserve([64, 64])
+    k = torch.zeros((2, 2, 3, 64), dtype=torch.float16, device=U.DEVICE)
+    one, q = k[:, :, :1].contiguous(), torch.zeros((2, 4, 64), dtype=torch.float16, device=U.DEVICE)
+    rope = binding.Rope([1.0], device=U.DEVICE)
+    at = torch.zeros((2, 3), dtype=torch.int32, device=U.DEVICE)
+    for bad in (k.float(), k.cpu(), k.bfloat16(), k[:, :1].contiguous(), k.transpose(1, 2).contiguous().transpose(1, 2), k[..., :32].contiguous()):
+        with pytest.raises(ValueError):
+            cache.append(bad, k)
+        with pytest.raises(ValueError):
+            cache.append(k, bad)
+    for kw in (dict(positions=at), dict(rope=rope, positions=at[:1].contiguous()), dict(rope=rope, positions=at.long()), dict(n_new=[1])):
+        with pytest.raises(ValueError):
+            cache.append(k, k, **kw)
+    for bad in (q.float(), q[:1].contiguous(), q.cpu(), q[..., ::2]):
+        with pytest.raises(ValueError):
+            cache.decode_attn(bad)
+        with pytest.raises(ValueError):
+            cache.decode_step(one, one, bad)
+        with pytest.raises(ValueError):
+            cache.decode_attn(q, bad)
+    slopes = torch.zeros(4, device=U.DEVICE)
+    for bad in (slopes[:3].contiguous(), slopes.cpu(), slopes.double()):
+        with pytest.raises(ValueError):
+            cache.decode_attn(q, slopes=bad)
+    with pytest.raises(ValueError):
+        cache.decode_step(k, one, q)
+    with pytest.raises(ValueError):
+        cache.evict([1])
+    with pytest.raises(ValueError):
+        cache.reserve([1])
+    with pytest.raises(binding.LogQuantError):
+        cache.decode_attn(q, window=-1)
+    assert cache.counts() == [0, 0]
