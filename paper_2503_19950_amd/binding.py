@@ -706,16 +706,19 @@ def _tensor(name, t, shape, dtype, device):
     return t.data_ptr()
 
 
-def _on_device(index, name, *args):
+def _on_device(index, f, *args):
     """An entry point on the current stream of device `index`, whichever device is current."""
-    f = getattr(_lib, name)
     if torch._C._cuda_getDevice() == index:
         st = f(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(index):
             st = f(*args, torch._C._cuda_getCurrentRawStream(index))
     if st != LQ_OK:
-        raise LogQuantError(st, name)
+        raise LogQuantError(st, f.__name__)
+
+
+_rotate, _init_paged, _append_paged = _lib.logquant_rotate, _lib.logquant_workspace_init_paged, _lib.logquant_append_paged
+_attn_paged, _step_paged, _evict_paged = _lib.logquant_decode_attn_paged, _lib.logquant_decode_step_paged, _lib.logquant_evict_paged
 
 
 class Rope:
@@ -727,6 +730,7 @@ class Rope:
         self.freq = torch.as_tensor(freq, dtype=torch.float64).to(self.device).contiguous()
         if self.freq.dim() != 1 or not len(self.freq):
             raise ValueError("freq: expected one frequency for every pair")
+        self.index = self.device.index
         self.c = lq_rope(2 * len(self.freq), int(interleaved), factor, self.freq.data_ptr())
         self._c = C.byref(self.c)
 
@@ -738,35 +742,35 @@ def rotate(rope, positions=None, q=None, k=None, q_out=None, k_out=None):
     x = q if q is not None else k
     if x is None:
         raise ValueError("rotate: no tensor")
-    if x.dim() not in (3, 4) or x.dtype not in (torch.float16, torch.bfloat16):
+    dtype, shape, device = x.dtype, x.shape, rope.device
+    B, L, d = shape[0], shape[2] if len(shape) == 4 else 1, shape[-1]
+    if len(shape) not in (3, 4) or (dtype is not torch.bfloat16 and dtype is not torch.float16):
         raise ValueError("rotate: expected fp16 or bf16 tensors of shape [B][H][L][d] or [B][H][d]")
-    B, L, d = x.shape[0], x.shape[2] if x.dim() == 4 else 1, x.shape[-1]
-    heads, at = [], []
-    for name, t, out in (("q", q, q_out), ("k", k, k_out)):
-        if t is None:
-            if out is not None:
-                raise ValueError("%s_out without %s" % (name, name))
-            heads.append(0)
-            at += [None, None]
-            continue
-        shape = torch.Size((B, t.shape[1] if t.dim() > 1 else 0, L, d) if t.dim() == 4 else (B, t.shape[1] if t.dim() > 1 else 0, d))
-        if L != 1 and t.dim() != 4:
-            raise ValueError("%s: expected [B][H][L][d]" % name)
-        src = _tensor(name, t, shape, x.dtype, rope.device)
-        if out is None:
-            out = torch.empty_like(t)
-        dst = _tensor(name + "_out", out, shape, x.dtype, rope.device)
-        heads.append(shape[1])
-        at += [src, dst]
-        if name == "q":
-            q_out = out
-        else:
-            k_out = out
-    p = None
+    Hq = Hkv = 0
+    at_q = at_q_out = at_k = at_k_out = at = None
+    if q is not None:
+        Hq = shape[1]
+        at_q = _tensor("q", q, shape, dtype, device)
+        if q_out is None:
+            q_out = torch.empty_like(q)
+        at_q_out = at_q if q_out is q else _tensor("q_out", q_out, shape, dtype, device)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        shape = k.shape
+        if len(shape) not in (3, 4) or shape[0] != B or shape[-1] != d or (shape[2] if len(shape) == 4 else 1) != L:
+            raise ValueError("k: expected [%d][Hkv][%d][%d]" % (B, L, d))
+        Hkv = shape[1]
+        at_k = _tensor("k", k, shape, dtype, device)
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        at_k_out = at_k if k_out is k else _tensor("k_out", k_out, shape, dtype, device)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
     if positions is not None:
-        p = _tensor("positions", positions, torch.Size((B,) if positions.dim() == 1 and L == 1 else (B, L)), torch.int32, rope.device)
-    _on_device(rope.device.index, "logquant_rotate", rope._c, B, L, heads[0], heads[1], d, LQ_BF16 if x.dtype is torch.bfloat16 else LQ_F16,
-               p, *at)
+        at = _tensor("positions", positions, (B,) if L == 1 and positions.dim() == 1 else (B, L), torch.int32, device)
+    _on_device(rope.index, _rotate, rope._c, B, L, Hq, Hkv, d, LQ_BF16 if dtype is torch.bfloat16 else LQ_F16, at, at_q, at_q_out, at_k,
+               at_k_out)
     return q_out, k_out
 
 
@@ -802,7 +806,7 @@ class DeviceCachePaged:
         self._cfg, self._c, self._ws = C.byref(cfg), C.byref(self.c), self.workspace.data_ptr()
         self._q_shape, self._token = torch.Size((B, cfg.Hq, cfg.d)), torch.Size((B, cfg.Hkv, 1, cfg.d))
         self._scores, self._scores_of = None, (0.0, 0, None)
-        _on_device(self._index, "logquant_workspace_init_paged", self._cfg, self._ws)
+        _on_device(self._index, _init_paged, self._cfg, self._ws)
 
     # ---- pages
     def set_pages(self, b, ids, spare=False):
@@ -895,13 +899,13 @@ class DeviceCachePaged:
         if n_new is not None and len(n_new) != c.B:
             raise ValueError("n_new: expected %d counts" % c.B)
         turn, at = self._turn(rope, positions, n)
-        _on_device(self._index, "logquant_append_paged", self._cfg, self._c, turn, at, k, v, _i32(n_new), n)
+        _on_device(self._index, _append_paged, self._cfg, self._c, turn, at, k, v, _i32(n_new), n)
 
     def decode_attn(self, q, out=None, softmax_scale=0.0, softcap=0.0, window=0, slopes=None):
         """q: [B][Hq][d]; rows of the batch that hold no token give zeros.  slopes: [Hq] fp32."""
         if out is None:
             out = torch.empty_like(q)
-        _on_device(self._index, "logquant_decode_attn_paged", self._cfg, self._c, self._how(softcap, window, slopes),
+        _on_device(self._index, _attn_paged, self._cfg, self._c, self._how(softcap, window, slopes),
                    _tensor("q", q, self._q_shape, self.dtype, self.device), softmax_scale,
                    _tensor("out", out, self._q_shape, self.dtype, self.device), self._ws)
         return out
@@ -912,7 +916,7 @@ class DeviceCachePaged:
         if out is None:
             out = torch.empty_like(q)
         turn, at = self._turn(rope, positions, 1)
-        _on_device(self._index, "logquant_decode_step_paged", self._cfg, self._c, turn, at, self._how(softcap, window, slopes),
+        _on_device(self._index, _step_paged, self._cfg, self._c, turn, at, self._how(softcap, window, slopes),
                    _tensor("k_new", k_new, self._token, self.dtype, self.device), _tensor("v_new", v_new, self._token, self.dtype, self.device),
                    _tensor("q", q, self._q_shape, self.dtype, self.device), softmax_scale,
                    _tensor("out", out, self._q_shape, self.dtype, self.device), self._ws)
@@ -926,4 +930,4 @@ class DeviceCachePaged:
         if len(keep) != self.cfg.B:
             raise ValueError("keep: expected %d counts" % self.cfg.B)
         self.reserve([x if n > x else 0 for n, x in zip(self.n, keep)], spare=True)
-        _on_device(self._index, "logquant_evict_paged", self._cfg, self._c, _i32(keep), recent, self._ws)
+        _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)

@@ -29,47 +29,50 @@ __device__ __forceinline__ uint16_t load2(__amdgpu_buffer_rsrc_t rs, int off) { 
 // token within its unit of 32 at position e of the eight that lane row a holds
 __device__ __forceinline__ int value_token(int a, int e) { return 16 * (e >> 2) + 4 * a + (e & 3); }
 
-// Channels c0 .. c0+7 of a key (offset `row` of rs), turned; angle: that token's.
-template <bool BF16>
-__device__ __forceinline__ u32x4 turned(__amdgpu_buffer_rsrc_t rs, int row, int c0, u32x4 x, const RopeArg& rope, const float2* angle) {
-  const int dims = rope.dims, half = dims / 2;
-  if (rope.interleaved) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if (c0 + 2 * w >= dims) break;
-      uint16_t p = (uint16_t)x[w], o = (uint16_t)(x[w] >> 16);
-      turn_pair<BF16>(p, o, angle[c0 / 2 + w]);
-      x[w] = p | (uint32_t)o << 16;
-    }
-    return x;
-  }
-  if (c0 >= dims) return x;
-  u32x4 y{0, 0, 0, 0};                       // the pairs' other halves
-  if (dims % 16 == 0) {
-    y = load16(rs, row + 2 * (c0 < half ? c0 + half : c0 - half));
-  } else {
+// How keys are turned: not at all; pairs of neighbours; pairs of halves that are whole pieces of 16 bytes; of halves that are not.
+enum Turn { NONE, NEIGHBOURS, HALVES, ODD };
+
+// The other halves of the pairs that channels c0 .. c0+7 of a key (offset `row` of rs) belong to.
+template <int TURN>
+__device__ __forceinline__ u32x4 other_halves(__amdgpu_buffer_rsrc_t rs, int row, int c0, int dims) {
+  const int half = dims / 2, nothing = 0x7FFFF000;
+  if constexpr (TURN == HALVES) return load16(rs, c0 < dims ? row + 2 * (c0 < half ? c0 + half : c0 - half) : nothing);
+  u32x4 y{0, 0, 0, 0};
+  if constexpr (TURN == ODD)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int c = c0 + e;
-      if (c < dims) y[e / 2] |= (uint32_t)load2(rs, row + 2 * (c < half ? c + half : c - half)) << (16 * (e & 1));
+      y[e / 2] |= (uint32_t)load2(rs, c < dims ? row + 2 * (c < half ? c + half : c - half) : nothing) << (16 * (e & 1));
     }
+  return y;
+}
+// Channels c0 .. c0+7 turned; y: other_halves; angle: that token's.  (The results of turn_pair, bit for bit.)
+template <bool BF16, int TURN>
+__device__ __forceinline__ u32x4 turned(int c0, u32x4 x, u32x4 y, int dims, const float2* angle) {
+  if constexpr (TURN == NEIGHBOURS) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint16_t p = (uint16_t)x[w], o = (uint16_t)(x[w] >> 16);
+      turn_pair<BF16>(p, o, angle[c0 / 2 + w]);
+      if (c0 + 2 * w < dims) x[w] = p | (uint32_t)o << 16;
+    }
+    return x;
   }
+  const int half = dims / 2;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int c = c0 + e, sh = 16 * (e & 1);
-    if (c >= dims) break;
-    const bool first = c < half;
-    uint16_t own = (uint16_t)(x[e / 2] >> sh), other = (uint16_t)(y[e / 2] >> sh);
-    const float2 cs = angle[first ? c : c - half];
-    uint16_t p = first ? own : other, o = first ? other : own;
-    turn_pair<BF16>(p, o, cs);
-    x[e / 2] = (x[e / 2] & ~(0xFFFFu << sh)) | (uint32_t)(first ? p : o) << sh;
+    const bool first = TURN == HALVES ? c0 < half : c < half;
+    const float2 cs = TURN == HALVES ? (angle + (first ? c0 : c0 - half))[e] : angle[first ? c : c - half];
+    const float own = t2f<BF16>((uint16_t)(x[e / 2] >> sh)), other = t2f<BF16>((uint16_t)(y[e / 2] >> sh));
+    const uint32_t z = f2t<BF16>(fmaf(own, cs.x, other * (first ? -cs.y : cs.y)));
+    if (c < dims) x[e / 2] = (x[e / 2] & ~(0xFFFFu << sh)) | z << sh;
   }
   return x;
 }
 
 // grid (units that a row's new tokens touch, shares of the kv heads, B)
-template <bool BF16, int D, int MODE, bool TURN>
+template <bool BF16, int D, int MODE, int TURN>
 __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPagedParams P, const Rows8<MODE> S) {
   (void)S;
   constexpr int ND = D / 32;
@@ -92,6 +95,29 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
         P.weights[((((int64_t)row.b * P.Hkv + head0 + x / 32) * P.max_pages) << P.log_p) + 32 * unit + x % 32] = 0.f;
   const int id = P.table[(int64_t)row.b * P.max_pages + (unit >> (P.log_p - 5))];
   if (!is_page(id, P.n_pages)) return;
+  // the first head's rows are under way while the angles are computed
+  __amdgpu_buffer_rsrc_t rk;
+  u32x4 k[2 * ND], y[ND];
+  uint32_t v[ND][8];
+  auto load_y = [&](int tile) {
+    if constexpr (TURN)
+#pragma unroll
+      for (int nd = 0; nd < ND; ++nd) y[nd] = other_halves<TURN>(rk, (16 * tile + lane % 16 - low) * (2 * D), 32 * nd + 8 * a, P.rope.dims);
+  };
+  auto load = [&](int h) {                                              // tokens outside low .. high - 1: zeros, not read
+    const int64_t from = (((int64_t)b * P.Hkv + h) * P.n_max + new0) * D;
+    rk = buffer(P.k_new + from, (high - low) * D * 2);
+    const __amdgpu_buffer_rsrc_t rv = buffer(P.v_new + from, (high - low) * D * 2);
+#pragma unroll
+    for (int x = 0; x < 2 * ND; ++x) k[x] = load16(rk, (16 * (x / ND) + lane % 16 - low) * (2 * D) + 2 * (32 * (x % ND) + 8 * a));
+    load_y(0);
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[nd][e] = load4(rv, (value_token(a, e) - low) * (2 * D) + 2 * (32 * nd + 2 * (lane % 16)));
+  };
+  int h = head0 + wave;
+  if (h < head1) load(h);
   __shared__ __align__(16) float2 cs[TURN ? 32 * PITCH : 1];
   if constexpr (TURN) {
     const int pairs = P.rope.dims / 2;
@@ -102,26 +128,15 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
     }
     __syncthreads();
   }
-  for (int h = head0 + wave; h < head1; h += WAVES) {
-    const int64_t from = (((int64_t)b * P.Hkv + h) * P.n_max + new0) * D;
-    // tokens outside low .. high - 1: zeros, not read
-    const __amdgpu_buffer_rsrc_t rk = buffer(P.k_new + from, (high - low) * D * 2), rv = buffer(P.v_new + from, (high - low) * D * 2);
+  for (; h < head1; h += WAVES) {
     const int64_t off = unit_offset(id, P.Hkv, h, P.log_p, unit, D);
-    u32x4 k[2 * ND];
-    uint32_t v[ND][8];
-#pragma unroll
-    for (int x = 0; x < 2 * ND; ++x) k[x] = load16(rk, (16 * (x / ND) + lane % 16 - low) * (2 * D) + 2 * (32 * (x % ND) + 8 * a));
-#pragma unroll
-    for (int nd = 0; nd < ND; ++nd)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[nd][e] = load4(rv, (value_token(a, e) - low) * (2 * D) + 2 * (32 * nd + 2 * (lane % 16)));
 #pragma unroll
     for (int x = 0; x < 2 * ND; ++x) {
       const int t = 16 * (x / ND) + lane % 16, c = 32 * (x % ND) + 8 * a;
+      if (x == ND) load_y(1);
       if (t < low || t >= high) continue;
-      u32x4 y = k[x];
-      if constexpr (TURN) y = turned<BF16>(rk, (t - low) * (2 * D), c, y, P.rope, cs + t * PITCH);
-      *reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8) = y;
+      if constexpr (TURN) k[x] = turned<BF16, TURN>(c, k[x], y[x % ND], P.rope.dims, cs + t * PITCH);
+      *reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8) = k[x];
     }
 #pragma unroll
     for (int nd = 0; nd < ND; ++nd) {
@@ -145,6 +160,7 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
         }
       }
     }
+    if (h + WAVES < head1) load(h + WAVES);
   }
 }
 
@@ -152,14 +168,20 @@ template <int MODE>
 hipError_t append_paged(const ShapePaged& s, const AppendPagedParams& p, const Rows8<MODE>& rows, dim3 grid, hipStream_t st) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * WAVES), 0, st, p, rows); };
   auto with = [&](auto t, auto turn) {
-    constexpr bool T = decltype(t)::value, TURN = decltype(turn)::value;
+    constexpr bool T = decltype(t)::value;
+    constexpr int TURN = decltype(turn)::value;
     if (s.d == 64) return go(append_paged_kernel<T, 64, MODE, TURN>);
     if (s.d == 96) return go(append_paged_kernel<T, 96, MODE, TURN>);
     go(append_paged_kernel<T, 128, MODE, TURN>);
   };
-  if (!p.rope.freq) with(std::false_type{}, std::false_type{});        // (the type does not matter)
-  else if (s.bf16) with(std::true_type{}, std::true_type{});
-  else with(std::false_type{}, std::true_type{});
+  auto with_type = [&](auto t) {
+    if (p.rope.interleaved) return with(t, std::integral_constant<int, NEIGHBOURS>{});
+    if (p.rope.dims % 16) return with(t, std::integral_constant<int, ODD>{});
+    with(t, std::integral_constant<int, HALVES>{});
+  };
+  if (!p.rope.freq) with(std::false_type{}, std::integral_constant<int, NONE>{});      // (the type does not matter)
+  else if (s.bf16) with_type(std::true_type{});
+  else with_type(std::false_type{});
   return launch_status("append_paged");
 }
 

@@ -9,10 +9,13 @@ namespace lq {
 // A workspace: counters and partial results of attention as for the 8-bit cache (Shape8 of the same heads), and of a weighted
 // cache behind them every query head's softmax reference and 1 / sum, and its logits by token, [B][Hq][cap] (attention), or
 // the slots of the tokens that stay, [B][Hkv][cap] (eviction).
+// Rows of more than EVICT_SHORT tokens are counted in memory: three histograms and what they say, and two counts for every
+// EVICT_PIECE tokens, of each kv head.
+constexpr int EVICT_SHORT = 16384, EVICT_BINS = 2048, EVICT_PIECE = 2048, EVICT_MEMORY = 3 * EVICT_BINS + 8;
 struct WorkspacePaged {
   int* counters;
   float *partials, *stats, *logits;
-  int* slots;
+  int *slots, *found;
   size_t bytes;
 };
 inline WorkspacePaged split_workspace(const ShapePaged& s, void* ws) {
@@ -30,6 +33,10 @@ inline WorkspacePaged split_workspace(const ShapePaged& s, void* ws) {
     w.logits = (float*)at;
     w.slots = (int*)at;
     at += (size_t)s.B * s.Hq * s.cap() * sizeof(float);
+    if (s.cap() > EVICT_SHORT) {
+      w.found = (int*)at;
+      at += (size_t)s.B * s.Hkv * (EVICT_MEMORY + 2 * ((s.cap() + EVICT_PIECE - 1) / EVICT_PIECE)) * sizeof(int);
+    }
   }
   w.bytes = (size_t)(at - (char*)ws);
   return w;
