@@ -70,6 +70,45 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
   const int heads = P.hb < P.gh - g * P.hb ? P.hb : P.gh - g * P.hb;
   const int64_t head0 = bh * P.gh + g * P.hb;
 
+  // ---- queries.  Their loads come first: loads arrive in order.
+  u32x4 q[SETS][ND];
+  constexpr int K_NEW = 16 * SETS, V_NEW = K_NEW + 1, ROWS = (V_NEW + 1 + NW - 1) / NW;
+  __shared__ __align__(16) uint16_t fresh[STEP ? (K_NEW + 2) * D : 1];  // step: queries, the new key (both turned) and value
+  // A step's rows go round the wavefronts, two channels a lane: a pair that turns, or two neighbours of the rest.
+  const int dims = STEP && P.rope.freq ? P.rope.dims : 0, pairs = dims / 2;
+  const int c0 = lane >= pairs || P.rope.interleaved ? 2 * lane : lane, c1 = lane >= pairs || P.rope.interleaved ? c0 + 1 : lane + pairs;
+  uint16_t x0[ROWS], x1[ROWS];
+  double freq = 0.0;
+  int position = n - 1;
+  if constexpr (STEP) {
+    if (lane < pairs) {
+      freq = P.rope.freq[lane];
+      if (P.rope.positions) position = P.rope.positions[b];
+    }
+#pragma unroll
+    for (int y = 0; y < ROWS; ++y) {
+      const int r = wave + y * NW;
+      if (r >= heads + 2 || 2 * lane >= D) break;
+      const uint16_t* from = r < heads ? P.q + (head0 + r) * D : (r == heads ? P.k_new : P.v_new) + bh * D;
+      x0[y] = from[r <= heads ? c0 : 2 * lane];
+      x1[y] = from[r <= heads ? c1 : 2 * lane + 1];
+    }
+  } else {
+    const __amdgpu_buffer_rsrc_t rs = buffer(P.q + head0 * D, heads * D * 2);              // absent heads: zeros
+#pragma unroll
+    for (int x = 0; x < SETS; ++x)
+#pragma unroll
+      for (int nd = 0; nd < ND; ++nd) q[x][nd] = load16(rs, (16 * x + head) * D * 2 + a * 16 + nd * 64);
+  }
+
+  float slope[SETS];                                                    // times log2(e)
+  if constexpr (MORE) {
+    const __amdgpu_buffer_rsrc_t rs = buffer(P.slopes + h * P.gh + g * P.hb, P.slopes ? heads * 4 : 0);
+#pragma unroll
+    for (int x = 0; x < SETS; ++x)
+      slope[x] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (16 * x + head) * 4, 0, 0)) * 1.44269504088896340736f;
+  }
+
   // ---- units of this wavefront: the i-th, counted from a place of the workgroup's own (in step, the workgroups of a launch
   // wait for the same memory channels where pages follow each other: lq_attn8.hip)
   typedef const int __attribute__((address_space(4))) * TablePtr;       // read by scalar loads
@@ -98,32 +137,21 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
 #pragma unroll
     for (int t = 0; t < NT; ++t) v[t] = load16(rs, t * 1024 + lane * 16);
   };
-  if (i < mine.stop) {
-    next = look(i);
-    load_k();
-    load_v();
-  }
+  next = look(i);                                                       // (a wavefront that has none reads nothing)
+  load_k();
+  load_v();
 
-  // ---- queries
-  u32x4 q[SETS][ND];
-  constexpr int K_NEW = 16 * SETS, V_NEW = K_NEW + 1;
-  __shared__ __align__(16) uint16_t fresh[STEP ? (K_NEW + 2) * D : 1];  // step: queries, the new key (turned) and value
   if constexpr (STEP) {
-    const int dims = P.rope.freq ? P.rope.dims : 0, pairs = dims / 2;
     float2 cs = make_float2(1.f, 0.f);
-    if (lane < pairs) cs = turn_of(P.rope.freq[lane], P.rope.positions ? P.rope.positions[b] : n - 1, P.rope.factor);
-    for (int r = wave; r < heads + 2; r += NW) {
-      const uint16_t* from = r < heads ? P.q + (head0 + r) * D : (r == heads ? P.k_new : P.v_new) + bh * D;
+    if (lane < pairs) cs = turn_of(freq, position, P.rope.factor);
+#pragma unroll
+    for (int y = 0; y < ROWS; ++y) {
+      const int r = wave + y * NW;
+      if (r >= heads + 2 || 2 * lane >= D) break;
       uint16_t* to = fresh + (r < heads ? r : r == heads ? K_NEW : V_NEW) * D;
-      const int turned = r <= heads ? dims : 0;
-      if (lane < turned / 2) {
-        const int c0 = P.rope.interleaved ? 2 * lane : lane, c1 = P.rope.interleaved ? c0 + 1 : lane + pairs;
-        uint16_t x0 = from[c0], x1 = from[c1];
-        turn_pair<BF16>(x0, x1, cs);
-        to[c0] = x0;
-        to[c1] = x1;
-      }
-      for (int c = turned + lane; c < D; c += 64) to[c] = from[c];
+      if (r <= heads && lane < pairs) turn_pair<BF16>(x0[y], x1[y], cs);
+      to[r <= heads ? c0 : 2 * lane] = x0[y];
+      to[r <= heads ? c1 : 2 * lane + 1] = x1[y];
     }
     __syncthreads();
 #pragma unroll
@@ -131,18 +159,15 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
 #pragma unroll
       for (int nd = 0; nd < ND; ++nd)
         q[x][nd] = 16 * x + head < heads ? *reinterpret_cast<const u32x4*>(fresh + (16 * x + head) * D + 32 * nd + 8 * a) : u32x4{0, 0, 0, 0};
-  } else {
-    const __amdgpu_buffer_rsrc_t rs = buffer(P.q + head0 * D, heads * D * 2);              // absent heads: zeros
-#pragma unroll
-    for (int x = 0; x < SETS; ++x)
-#pragma unroll
-      for (int nd = 0; nd < ND; ++nd) q[x][nd] = load16(rs, (16 * x + head) * D * 2 + a * 16 + nd * 64);
   }
-  float slope[SETS];                                                    // times log2(e)
-  if constexpr (MORE) {
+  // What came before the keys is there from here on (the compiler, which counts loads, would wait for it, and with it for all
+  // loads under way, in every round of the loop: 131072 tokens x 8 kv heads TODO us).
 #pragma unroll
-    for (int x = 0; x < SETS; ++x)
-      slope[x] = P.slopes && 16 * x + head < heads ? P.slopes[h * P.gh + g * P.hb + 16 * x + head] * 1.44269504088896340736f : 0.f;
+  for (int x = 0; x < SETS; ++x) {
+    if constexpr (!STEP)
+#pragma unroll
+      for (int nd = 0; nd < ND; ++nd) asm volatile("" : "+v"(q[x][nd]));
+    if constexpr (MORE) asm volatile("" : "+v"(slope[x]));
   }
 
   f32x4 acc[SETS][NT];
@@ -222,6 +247,8 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
           v[t][w] &= (t0 >= low && t0 < high ? 0xFFFFu : 0u) | (t0 + 1 >= low && t0 + 1 < high ? 0xFFFF0000u : 0u);
         }
     }
+    __amdgpu_buffer_rsrc_t logits;
+    if constexpr (MORE) logits = buffer(P.logits + ((bh * (P.max_pages << (P.log_p - 5)) + u) * (2 * P.gh) + g * P.hb) * 16, P.logits ? P.gh * 128 : 0);
     float z[SETS][8];
 #pragma unroll
     for (int x = 0; x < SETS; ++x) {
@@ -243,12 +270,10 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
           const int t = 16 * (e / 4) + 4 * a + e % 4;
           if (t < low || t >= high) z[x][e] = -INFINITY;
         }
-      if constexpr (MORE) {
-        if (P.logits && 16 * x + head < heads) {
-          float* to = P.logits + (head0 + 16 * x + head) * ((int64_t)P.max_pages << P.log_p) + 32 * (int64_t)u + 4 * a;
-          *reinterpret_cast<f32x4*>(to) = f32x4{z[x][0], z[x][1], z[x][2], z[x][3]};
-          *reinterpret_cast<f32x4*>(to + 16) = f32x4{z[x][4], z[x][5], z[x][6], z[x][7]};
-        }
+      if constexpr (MORE) {                                             // for the weights (heads that are not there: not stored)
+        const int at = 16 * x + head < heads ? (16 * x + head) * 64 + 16 * a : 0x7FFFF000;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{z[x][0], z[x][1], z[x][2], z[x][3]}), logits, at, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{z[x][4], z[x][5], z[x][6], z[x][7]}), logits, at, P.gh * 64, 0);
       }
       float top = z[x][0];
 #pragma unroll

@@ -32,10 +32,11 @@ __global__ void __launch_bounds__(256) weights_kernel(const WeightsParams P, con
   const int t = first_seen(row.n, P.window) / 32 * 32 + ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4;
   if (t >= row.n) return;
   const int64_t head0 = ((int64_t)b * P.Hkv + h) * P.gh;
+  const float* at = P.logits + (((int64_t)b * P.Hkv + h) * (P.cap / 16) + t / 16) * (P.gh * 16) + t % 16;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int g = 0; g < P.gh; ++g) {
     const float m = P.stats[2 * (head0 + g)], inv = P.stats[2 * (head0 + g) + 1];
-    const f32x4 z = *reinterpret_cast<const f32x4*>(P.logits + (head0 + g) * P.cap + t);
+    const f32x4 z = *reinterpret_cast<const f32x4*>(at + 16 * g);
     if (inv > 0.f)                                     // (else nothing had weight)
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(__builtin_amdgcn_exp2f(z[e] - m), inv, sum[e]);

@@ -7,7 +7,7 @@
 namespace lq {
 
 // A workspace: counters and partial results of attention as for the 8-bit cache (Shape8 of the same heads), and of a weighted
-// cache behind them every query head's softmax reference and 1 / sum, and its logits by token, [B][Hq][cap] (attention), or
+// cache behind them every query head's softmax reference and 1 / sum, and the logits, [B][Hkv][cap / 16][Hq / Hkv][16] (attention), or
 // the slots of the tokens that stay, [B][Hkv][cap] (eviction).
 // Rows of more than EVICT_SHORT tokens are counted in memory: three histograms and what they say, and two counts for every
 // EVICT_PIECE tokens, of each kv head.
