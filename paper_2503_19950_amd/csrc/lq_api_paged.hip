@@ -80,10 +80,9 @@ static bool alike(const RowList& rows) {
 // rows: n tokens each, the step's among them.
 static lq_status attend_paged(const ShapePaged& s, const lq_cache_paged& c, RowList* rows, const ScoresArg& scores, const NewToken* step,
                               const void* q, void* out, void* workspace, hipStream_t stream) {
-  Plan8 plan;
-  int most;
-  const bool alone = plan_paged(s, scores.window, step, alike(*rows), rows->e, rows->n, &plan, &most);
-  return launch_attn_paged(s, c, scores, q, out, workspace, plan, step, most, rows->arg(c.seq_state, alone), stream) == hipSuccess ? LQ_OK
+  PlanPaged plan;
+  const bool alone = plan_paged(s, scores.window, step, alike(*rows), rows->e, rows->n, &plan);
+  return launch_attn_paged(s, c, scores, q, out, workspace, plan, step, rows->arg(c.seq_state, alone), stream) == hipSuccess ? LQ_OK
                                                                                                                                    : LQ_ERR_HIP;
 }
 

@@ -13,6 +13,7 @@
 #include "lq_attn_paged_args.h"
 #include "lq_attn_parts.h"
 #include "lq_internal.h"
+#include "lq_weights.h"
 
 namespace lq {
 
@@ -30,6 +31,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
   (void)S;
   constexpr int ND = D / 32, NT = D / 16, UNIT = 32 * D;                // UNIT: elements of a unit's keys, or values
   extern __shared__ __align__(16) float o_lds[];                        // lds_bytes8
+  float* z_lds = o_lds + lds_bytes8(NW, P.hb, D) / 4;                   // with P.weights: logits, as they lie in memory
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int a = lane / 16, head = lane % 16;
   const int per_row = P.Hkv * P.groups;                                 // items of a row
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
         q[x][nd] = 16 * x + head < heads ? *reinterpret_cast<const u32x4*>(fresh + (16 * x + head) * D + 32 * nd + 8 * a) : u32x4{0, 0, 0, 0};
   }
   // What came before the keys is there from here on (the compiler, which counts loads, would wait for it, and with it for all
-  // loads under way, in every round of the loop: 131072 tokens x 8 kv heads TODO us).
+  // loads under way, in every round of the loop).
 #pragma unroll
   for (int x = 0; x < SETS; ++x) {
     if constexpr (!STEP)
@@ -271,6 +273,13 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
           if (t < low || t >= high) z[x][e] = -INFINITY;
         }
       if constexpr (MORE) {                                             // for the weights (heads that are not there: not stored)
+        if (P.weights) {
+          if (16 * x + head < heads) {
+            float* to = z_lds + ((u - mine.seen / 32) * 2 * heads + 16 * x + head) * 16 + 4 * a;
+            *reinterpret_cast<f32x4*>(to) = f32x4{z[x][0], z[x][1], z[x][2], z[x][3]};
+            *reinterpret_cast<f32x4*>(to + 16 * heads) = f32x4{z[x][4], z[x][5], z[x][6], z[x][7]};
+          }
+        }
         const int at = 16 * x + head < heads ? (16 * x + head) * 64 + 16 * a : 0x7FFFF000;
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{z[x][0], z[x][1], z[x][2], z[x][3]}), logits, at, 0, 0);
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{z[x][4], z[x][5], z[x][6], z[x][7]}), logits, at, P.gh * 64, 0);
@@ -297,20 +306,32 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
     load_v();
   }
 
+  __shared__ float2 stats[MORE ? 16 * SETS : 1];
   join_parts<D, NW, SETS>(o_lds, P.hb, heads, part, parts, first_slot, P.counters + (int64_t)(b * per_row + j) * CTR8, P.partials, acc, m, l,
                           [&](int hd, int c, f32x4 o, float top, float sum) {
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     *reinterpret_cast<u32x2*>(P.out + (head0 + hd) * D + c) =
         u32x2{pair_as<BF16>(o[0] * inv, o[1] * inv), pair_as<BF16>(o[2] * inv, o[3] * inv)};
     if constexpr (MORE)
-      if (P.stats && c == 0) *reinterpret_cast<float2*>(P.stats + 2 * (head0 + hd)) = make_float2(top, inv);
+      if (c == 0) {
+        stats[hd] = make_float2(top, inv);
+        if (P.stats) *reinterpret_cast<float2*>(P.stats + 2 * (head0 + hd)) = make_float2(top, inv);
+      }
   });
+  if constexpr (MORE) {
+    if (!P.weights) return;                            // (else parts == 1 and groups == 1)
+    __syncthreads();
+    const int first = mine.seen / 32 * 32;
+    float* w = P.weights + (((int64_t)rb * P.Hkv + h) * P.max_pages << P.log_p);
+    for (int t = first + 4 * threadIdx.x; t < n; t += 256 * NW)
+      add_weights<STEP>(w + t, t, n, heads, [&](int g) { return stats[g]; }, z_lds + (t - first) / 16 * (16 * heads) + t % 16);
+  }
 }
 
 template <int MODE, bool STEP, bool MORE>
 hipError_t attn_paged(const ShapePaged& s, const AttnPagedParams& p, const Rows8<MODE>& rows, const Plan8& plan, hipStream_t st) {
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(64 * plan.waves), lds_bytes8(plan.waves, plan.hb, s.d), st, p, rows);
+    hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(64 * plan.waves), lds_bytes8(plan.waves, plan.hb, s.d) + p.logits_lds, st, p, rows);
   };
   auto with = [&](auto bf16, auto waves, auto sets) {
     constexpr bool T = decltype(bf16)::value;

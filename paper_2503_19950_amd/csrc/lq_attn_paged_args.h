@@ -12,7 +12,9 @@ struct AttnPagedParams {
   const uint16_t *k_new, *v_new;             // step
   RopeArg rope;
   const float* slopes;
-  float *logits, *stats;                     // of a weighted cache, else null
+  float *logits, *stats;                     // of a weighted cache whose items are split: what weights_kernel reads; else null
+  float* weights;                            // of a weighted cache whose items are not, else null
+  int logits_lds;                            // bytes of logits in LDS, for them
   int* counters;
   float* partials;
   const Row8* rows;

@@ -95,9 +95,9 @@ constexpr int MAX_PARTS8 = 512;
 // two workgroups at any size (524288 tokens, 134 MB, 41.2 and 44.3; 94000 tokens, 24 MB, 17.7 and 22.1).
 inline int head_groups8(const Shape8& s, bool large) { return (s.gh + (large ? 31 : 15)) / (large ? 32 : 16); }
 inline size_t counter_bytes8(const Shape8& s) { return (size_t)s.B * s.Hkv * head_groups8(s, false) * CTR8 * sizeof(int); }
-inline int partial_floats8(int hb, int d) { return hb * (d + 4); }   // o, then m and l, padded to 16 bytes
+LQ8_HD int partial_floats8(int hb, int d) { return hb * (d + 4); }   // o, then m and l, padded to 16 bytes
 // LDS of a workgroup: each wavefront's results of a set of heads, or a join's (o, m and l of a share for every thread).
-inline int lds_bytes8(int waves, int hb, int d) {
+LQ8_HD int lds_bytes8(int waves, int hb, int d) {
   const int merge = waves * partial_floats8(hb < 16 ? hb : 16, d), join = waves * 64 * 6;
   return (merge > join ? merge : join) * (int)sizeof(float);
 }

@@ -58,9 +58,8 @@ struct NewToken {      // of a step
   const void *k, *v;
   RopeArg rope;
 };
-// most: the most tokens of a row that get weight
 hipError_t launch_attn_paged(const ShapePaged& s, const lq_cache_paged& c, const ScoresArg& scores, const void* q, void* out, void* ws,
-                             const Plan8& plan, const NewToken* step, int most, const RowArg8& rows, hipStream_t st);
+                             const PlanPaged& plan, const NewToken* step, const RowArg8& rows, hipStream_t st);
 // Entries of `rows` that are evicted from, `count` of them: n, x = tokens that stay.
 hipError_t launch_evict_paged(const ShapePaged& s, const lq_cache_paged& c, int recent, int most_kept, void* ws, const RowArg8& rows,
                               int count, hipStream_t st);

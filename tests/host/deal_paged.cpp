@@ -28,7 +28,7 @@ int main() {
   std::mt19937 rng(20261208);
   auto in = [&](int a, int b) { return (int)(a + rng() % (unsigned)(b - a + 1)); };
   auto log_in = [&](int b) { return (int)exp2(std::uniform_real_distribution<>(0, log2(b + 1.0))(rng)) - 1; };
-  long split = 0, sets = 0, wide = 0, windows = 0;
+  long split = 0, sets = 0, wide = 0, windows = 0, in_lds = 0;
   for (int the_case = 0; the_case < 3000; ++the_case) {
     ShapePaged s{};
     const int ds[] = {64, 96, 128}, Ps[] = {32, 64, 128}, ghs[] = {1, 2, 3, 4, 7, 8, 16, 17, 24, 32, 33, 71};
@@ -53,15 +53,27 @@ int main() {
     }
     std::vector<int> lengths(s.B);
     for (int b = 0; b < s.B; ++b) lengths[b] = rows[b].n;
-    Plan8 p;
-    int most;
+    PlanPaged plan;
+    s.weighted = in(0, 1);
     bool same = true;
     for (int b = 1; b < s.B; ++b) same = same && lengths[b] == lengths[0];
-    same = plan_paged(s, window, step, same, rows.data(), s.B, &p, &most);
+    same = plan_paged(s, window, step, same, rows.data(), s.B, &plan);
+    const Plan8 p = plan.deal;
     const int sets_of = p.hb > 16 ? 2 : 1, staged = step ? (16 * sets_of + 2) * s.d * 2 : 0;
     CHECK(lds_bytes8(p.waves, p.hb, s.d) + staged <= 65536);
     CHECK(p.waves == 4 || (p.hb <= 16 && (p.waves == 8 || (p.waves == 16 && !same && s.d == 64))));
     CHECK(p.hb <= 32 && p.groups * p.hb >= s.gh && (p.groups - 1) * p.hb < s.gh);
+    // logits in LDS: room for every row's, of items that are neither split nor shared, and a second workgroup of 4 wavefronts
+    if (plan.logits_lds) {
+      CHECK(s.weighted && p.groups == 1);
+      for (Row8& r : rows) {
+        const PartPaged all = part_paged(r.n, window, 0, 1);
+        CHECK(r.parts == 1 && (int64_t)(all.stop - all.pos) * 32 * s.gh * 4 <= plan.logits_lds);
+      }
+      const int all = lds_bytes8(p.waves, p.hb, s.d) + staged + 512 + plan.logits_lds;
+      CHECK(all <= LDS_OF_CU && (p.waves > 4 || 2 * all <= LDS_OF_CU));
+      ++in_lds;
+    }
     const int per_row = s.Hkv * p.groups;
     std::set<int> slots;
     std::map<int, int> row_of;
@@ -114,6 +126,6 @@ int main() {
       CHECK(off / ((int64_t)s.Hkv * s.P * s.d) == id && off / (s.P * s.d) % s.Hkv == h && off / (32 * s.d) % (s.P / 32) == u % (s.P / 32));
     }
   }
-  printf("%ld parts, %ld plans of two sets, %ld of more than 4 wavefronts, %ld rows behind a window\n", split, sets, wide, windows);
-  return split > 1000 && sets > 50 && wide > 50 && windows > 1000 ? 0 : 1;
+  printf("%ld parts, %ld plans of two sets, %ld of more than 4 wavefronts, %ld rows behind a window, %ld with logits in LDS\n", split, sets, wide, windows, in_lds);
+  return in_lds > 100 && split > 1000 && sets > 50 && wide > 50 && windows > 1000 ? 0 : 1;
 }

@@ -138,6 +138,40 @@ def test_weights_add_up(how, heads, dtype):
         assert torch.equal(now[0, b, :, cache.n[b]:], untouched[0, b, :, cache.n[b]:])
 
 
+# logits in LDS: rows of one length in workgroups of 4 wavefronts, of different lengths in larger ones, up to what a compute unit has;
+# through memory: longer rows, shared kv heads, split items
+@pytest.mark.parametrize("lengths,heads,d", [([500] * 40, (32, 8), 64), ([4096 - 61 * b % 3000 for b in range(36)], (32, 8), 128),
+                                             ([1 + 37 * b % 700 for b in range(40)], (40, 8), 96), ([3000 - 90 * b for b in range(20)], (64, 16), 64),
+                                             ([200] * 33, (8, 8), 96), ([700] * 9, (68, 2), 64), ([9000, 50], (4, 2), 64),
+                                             ([4500] * 40, (32, 8), 64)])
+@pytest.mark.parametrize("window", [0, 90])
+def test_weights_by_every_route(lengths, heads, d, window):
+    Hq, Hkv = heads
+    B, dtype = len(lengths), "f16"
+    cache, model = _filled(31, lengths, Hq, Hkv, d, 32, dtype, weighted=True)
+    untouched = cache.weights.view(torch.int32).clone()
+    q = U.rows(1, B, Hq, d, dtype=dtype)
+    out = cache.decode_attn(q.to(U.DEVICE), window=window)
+    for b in range(4, B - 2):                                            # (some rows are enough)
+        model.K[b], model.V[b] = model.K[b][:, :0], model.V[b][:, :0]
+    some = [b for b in range(B) if 4 <= b < B - 2]
+    model.check_output(out, q, window=window, weights=U.live_weights(cache), skip=some)
+    now = cache.weights.view(torch.int32)
+    for b in range(B):
+        assert torch.equal(now[0, b, :, cache.n[b]:], untouched[0, b, :, cache.n[b]:])
+        if window and cache.n[b] > window:
+            assert (now[0, b, :, :cache.n[b] - window] == 0).all()
+        # all of a head's probabilities, whatever their number: each is off by less than 2^-20 of itself, as are the sums
+        w = cache.weights[0, b, :, :cache.n[b]].double().sum(-1)
+        assert (w - Hq / Hkv).abs().max() < 2.0 ** -18 * Hq / Hkv
+    K, V = U.rows(2, B, Hkv, 1, d, dtype=dtype), U.rows(3, B, Hkv, 1, d, dtype=dtype)
+    again = cache.decode_step(K.to(U.DEVICE), V.to(U.DEVICE), q.to(U.DEVICE), window=window)
+    assert torch.isfinite(again).all()
+    for b in range(B):
+        w = cache.weights[0, b, :, :cache.n[b]].double().sum(-1)
+        assert (w - 2 * Hq / Hkv).abs().max() < 2.0 ** -17 * Hq / Hkv
+
+
 def test_a_cache_without_pages_of_some_rows_weighs_nothing():
     cache, model = _filled(19, [70, 40], 2, 1, 64, 32, "f16", weighted=True)
     cache.table[0, 0] = -1
