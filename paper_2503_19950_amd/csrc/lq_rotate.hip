@@ -1,8 +1,12 @@
 // Rotary positions of queries and keys.
 //
-// Bound by the bytes: a workgroup takes up to 16 tokens, computes their cosines and sines once, into LDS, and turns these
-// tokens' rows of all heads (or of a share of them, where tokens are few) with them.  A thread holds both halves of eight
-// pairs, or four pairs of neighbours, so that a row may be written where it was read.
+// Bound by the bytes.  A lane has 16 bytes of a row, a row lies within a wavefront, and a workgroup has up to T tokens of all
+// heads (or of a share of them, where tokens are few), head by head: consecutive tokens of a head are 8 KB in one stretch, and a
+// lane's token and channels stay the same, so that its cosines and sines are in registers, computed once by the workgroup
+// together.  The other halves of a lane's pairs come from the lane that has them; all of a row is read before any of it is
+// written, so that a row may be written where it was read.
+// 32768 tokens x 40 heads, d = 128, bf16 (671 MB): 130 us (4 and 8 heads under way a lane: 132 and 138; without
+// the stores' way past the caches 139); a copy of as much takes 130.
 #include "lq_internal.h"
 #include "lq_paged.h"
 #include "lq_quant8.h"
@@ -11,95 +15,119 @@ namespace lq {
 
 namespace {
 
-constexpr int TOKENS = 16, PITCH = 66;       // tokens of a workgroup; pairs from one token's angles to the next (64 and padding)
+constexpr int WAVES = 8;
 
 struct RotateParams {
   const uint16_t *q, *k;
   uint16_t *q_out, *k_out;
   RopeArg rope;
   int L, Hq, Hkv, heads;                     // Hq, Hkv: 0 for a tensor that is not wanted; heads: of a workgroup
-  int log_t;                                 // tokens of a workgroup
+  int tokens;                                // of a workgroup
 };
 
-// VECTOR: the rotated channels and their halves are whole pieces of 16 bytes
-template <bool BF16, int D, bool VECTOR>
-__global__ void __launch_bounds__(256) rotate_kernel(const RotateParams P) {
-  __shared__ __align__(16) float2 cs[TOKENS * PITCH];
-  const int b = blockIdx.z, tokens = 1 << P.log_t, t0 = (int)blockIdx.x << P.log_t, here = P.L - t0 < tokens ? P.L - t0 : tokens;
-  const int dims = P.rope.dims, pairs = dims / 2;
-  for (int x = threadIdx.x; x < here * pairs; x += 256) {
-    const int t = x / pairs, i = x - t * pairs;
-    const int position = P.rope.positions ? P.rope.positions[(int64_t)b * P.L + t0 + t] : t0 + t;
-    cs[t * PITCH + i] = turn_of(P.rope.freq[i], position, P.rope.factor);
+// How pairs lie: neighbours; halves that are whole pieces of 16 bytes; halves that are not.
+enum Pairs { NEIGHBOURS, HALVES, ODD };
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)v); }
+// Eight channels from `shift` channels (0 .. 7) into lo on, hi behind it.
+__device__ __forceinline__ u32x4 eight_from(u32x4 lo, u32x4 hi, int shift) {
+  u32x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {              // word e of (lo, hi) >> 16 * shift
+    const int s = shift / 2;
+    auto word = [&](int i) { return i < 4 ? lo[i] : i < 8 ? hi[i - 4] : 0u; };
+    uint32_t a = 0, b = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (w == s) {
+        a = word(e + w);
+        b = word(e + w + 1);
+      }
+    y[e] = shift & 1 ? a >> 16 | b << 16 : a;
   }
-  __syncthreads();
-  // a row is `turning` pieces that turn (VECTOR: 8 pairs or 4 pairs of neighbours, else a pair) and the pieces behind them
-  const bool side = P.rope.interleaved;
-  const int turning = VECTOR ? (side ? dims / 8 : dims / 16) : pairs, pieces = turning + (VECTOR ? (D - dims) / 8 : D - dims);
-  const int rows_at_once = 256 / pieces, first = threadIdx.x / pieces, piece = threadIdx.x - first * pieces;
-  if (first >= rows_at_once) return;
+  return y;
+}
+
+template <bool BF16, int D, int PAIRS>
+__global__ void __launch_bounds__(64 * WAVES) rotate_kernel(const RotateParams P) {
+  constexpr int PIECES = D / 8, ROWS = 64 / PIECES;      // of a row; of a wavefront
+  constexpr int AHEAD = 2, PITCH = D / 2 + 2;
+  __shared__ __align__(16) float2 angles[WAVES * ROWS * PITCH];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.z;
+  const int dims = P.rope.dims, half = dims / 2, t0 = (int)blockIdx.x * P.tokens, here = P.L - t0 < P.tokens ? P.L - t0 : P.tokens;
+  const int row = wave * ROWS + lane / PIECES, c0 = lane % PIECES * 8;
+  const int at_once = WAVES * ROWS / P.tokens, t = row % P.tokens;       // heads
+  const bool mine = lane < ROWS * PIECES && row < at_once * P.tokens && t < here;
   const int head0 = blockIdx.y * P.heads, head1 = head0 + P.heads < P.Hq + P.Hkv ? head0 + P.heads : P.Hq + P.Hkv;
-  const int rows = (head1 - head0) << P.log_t;
-  const bool turns = piece < turning;
-  const int c0 = !turns ? dims + (piece - turning) * (VECTOR ? 8 : 1) : side ? piece * (VECTOR ? 8 : 2) : piece * (VECTOR ? 8 : 1);
-  const int c1 = VECTOR ? c0 + pairs : side ? c0 + 1 : c0 + pairs;        // the pairs' other halves (VECTOR and side: in the same piece)
-  auto row_of = [&](int r, bool out) -> uint16_t* {
-    const int head = head0 + (r >> P.log_t), t = t0 + (r & (tokens - 1));
+  auto place = [&](int head, bool out) -> uint16_t* {
     const uint16_t* base = head < P.Hq ? (out ? P.q_out : P.q) : out ? P.k_out : P.k;
     const int64_t at = head < P.Hq ? (int64_t)b * P.Hq + head : (int64_t)b * P.Hkv + head - P.Hq;
-    return const_cast<uint16_t*>(base) + (at * P.L + t) * D;
+    return const_cast<uint16_t*>(base) + (at * P.L + t0 + t) * D + c0;
   };
-  constexpr int AHEAD = 4;                               // rows under way at a time
-  for (int r0 = first; r0 < rows; r0 += AHEAD * rows_at_once) {
-    u32x4 x[AHEAD], y[AHEAD];
-    uint16_t x1[AHEAD], y1[AHEAD];
+  u32x4 x[AHEAD];
+  auto load = [&](int h) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int r = r0 + j * rows_at_once;
-      if (r >= rows || (r & (tokens - 1)) >= here) continue;
-      const uint16_t* from = row_of(r, false);
-      if constexpr (VECTOR) {
-        x[j] = *reinterpret_cast<const u32x4*>(from + c0);
-        if (turns && !side) y[j] = *reinterpret_cast<const u32x4*>(from + c1);
-      } else {
-        x1[j] = from[c0];
-        if (turns) y1[j] = from[c1];
-      }
+      x[j] = u32x4{0, 0, 0, 0};
+      if (mine && h + j * at_once < head1) x[j] = *reinterpret_cast<const u32x4*>(place(h + j * at_once, false));
     }
+  };
+  int h = head0 + row / P.tokens;
+  load(h);
+  for (int i = threadIdx.x; i < here * half; i += 64 * WAVES) {
+    const int s = i / half, p = i - s * half;
+    const int position = P.rope.positions ? P.rope.positions[(int64_t)b * P.L + t0 + s] : t0 + s;
+    angles[s * PITCH + p] = turn_of(P.rope.freq[p], position, P.rope.factor);
+  }
+  __syncthreads();
+  // of the lane's pairs, four or eight: the sine's sign is that of the other half in the result
+  float co[8], si[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int c = c0 + e;
+    const bool first = PAIRS == NEIGHBOURS ? !(e & 1) : c < half;
+    const float2 cs = angles[(mine && c < dims ? t * PITCH + (PAIRS == NEIGHBOURS ? c / 2 : first ? c : c - half) : 0)];
+    co[e] = cs.x;
+    si[e] = first ? -cs.y : cs.y;
+  }
+  // lanes that have the other halves
+  const int q = half / 8, shift = half % 8, up = lane + q, down = lane - q - (shift ? 1 : 0);
+  for (; h - row / P.tokens < head1; h += AHEAD * at_once) {             // (wavefronts stay together)
+    u32x4 z[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int r = r0 + j * rows_at_once;
-      if (r >= rows || (r & (tokens - 1)) >= here) continue;
-      uint16_t* to = row_of(r, true);
-      const float2* angle = cs + (r & (tokens - 1)) * PITCH;
-      if constexpr (VECTOR) {
-        if (turns && side) {
+      u32x4 y{0, 0, 0, 0}, y2{0, 0, 0, 0};                               // the other halves of first and of second ones
+      if constexpr (PAIRS == HALVES) {
+        const int who = c0 < half ? up : down;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint16_t p = (uint16_t)x[j][w], o = (uint16_t)(x[j][w] >> 16);
-            turn_pair<BF16>(p, o, angle[c0 / 2 + w]);
-            x[j][w] = p | (uint32_t)o << 16;
-          }
-        } else if (turns) {
+        for (int w = 0; w < 4; ++w) y[w] = from_lane(x[j][w], who);
+      }
+      if constexpr (PAIRS == ODD) {
+        u32x4 n[4];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint16_t p = (uint16_t)x[j][w], o = (uint16_t)y[j][w], p1 = (uint16_t)(x[j][w] >> 16), o1 = (uint16_t)(y[j][w] >> 16);
-            turn_pair<BF16>(p, o, angle[c0 + 2 * w]);
-            turn_pair<BF16>(p1, o1, angle[c0 + 2 * w + 1]);
-            x[j][w] = p | (uint32_t)p1 << 16;
-            y[j][w] = o | (uint32_t)o1 << 16;
-          }
-          *reinterpret_cast<u32x4*>(to + c1) = y[j];
+        for (int w = 0; w < 4; ++w) {
+          n[0][w] = from_lane(x[j][w], up);
+          n[1][w] = from_lane(x[j][w], up + 1);
+          n[2][w] = from_lane(x[j][w], down);
+          n[3][w] = from_lane(x[j][w], down + 1);
         }
-        *reinterpret_cast<u32x4*>(to + c0) = x[j];
-      } else {
-        if (turns) {
-          turn_pair<BF16>(x1[j], y1[j], angle[piece]);
-          to[c1] = y1[j];
-        }
-        to[c0] = x1[j];
+        y = eight_from(n[0], n[1], shift);
+        y2 = shift ? eight_from(n[2], n[3], 8 - shift) : n[2];
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t o = PAIRS == NEIGHBOURS ? x[j][w] >> 16 | x[j][w] << 16 : PAIRS == HALVES ? y[w]
+                           : ((c0 + 2 * w < half ? y[w] : y2[w]) & 0xFFFFu) | ((c0 + 2 * w + 1 < half ? y[w] : y2[w]) & 0xFFFF0000u);
+        const uint32_t lo = f2t<BF16>(fmaf(t2f<BF16>((uint16_t)x[j][w]), co[2 * w], t2f<BF16>((uint16_t)o) * si[2 * w]));
+        const uint32_t hi = f2t<BF16>(fmaf(t2f<BF16>((uint16_t)(x[j][w] >> 16)), co[2 * w + 1], t2f<BF16>((uint16_t)(o >> 16)) * si[2 * w + 1]));
+        z[j][w] = (c0 + 2 * w < dims ? lo : x[j][w] & 0xFFFFu) | (c0 + 2 * w + 1 < dims ? hi << 16 : x[j][w] & 0xFFFF0000u);
       }
     }
+    const int at = h;
+    load(h + AHEAD * at_once);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (mine && at + j * at_once < head1) __builtin_nontemporal_store(z[j], reinterpret_cast<u32x4*>(place(at + j * at_once, true)));
   }
 }
 
@@ -107,24 +135,27 @@ __global__ void __launch_bounds__(256) rotate_kernel(const RotateParams P) {
 
 hipError_t launch_rotate(const RopeArg& rope, int B, int L, int Hq, int Hkv, int d, bool bf16, const void* q, void* q_out, const void* k,
                          void* k_out, hipStream_t st) {
-  int log_t = 0;
-  while (log_t < 4 && 1 << log_t < L) ++log_t;
-  const int chunks = (int)(((int64_t)L + (1 << log_t) - 1) >> log_t), heads = (q ? Hq : 0) + (k ? Hkv : 0);
+  const int rows = WAVES * (64 / (d / 8)), tokens = L < rows ? L : rows, heads = (q ? Hq : 0) + (k ? Hkv : 0);
+  const int chunks = (int)(((int64_t)L + tokens - 1) / tokens);
   // all heads share a workgroup's angles where there are workgroups enough
   int shares = 1;
-  while (shares < heads && (int64_t)chunks * B * shares < 1024) shares *= 2;
+  while (shares < heads && (int64_t)chunks * B * shares < 512) shares *= 2;
   shares = shares < heads ? shares : heads;
   const int per = (heads + shares - 1) / shares;
-  const RotateParams p{(const uint16_t*)q, (const uint16_t*)k, (uint16_t*)q_out, (uint16_t*)k_out, rope, L, q ? Hq : 0, k ? Hkv : 0, per, log_t};
-  const bool vector = rope.interleaved ? rope.dims % 8 == 0 : rope.dims % 16 == 0;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks, (heads + per - 1) / per, B), dim3(256), 0, st, p); };
-  auto with = [&](auto t, auto v) {
-    constexpr bool T = decltype(t)::value, V = decltype(v)::value;
-    if (d == 64) return go(rotate_kernel<T, 64, V>);
-    if (d == 96) return go(rotate_kernel<T, 96, V>);
-    go(rotate_kernel<T, 128, V>);
+  const RotateParams p{(const uint16_t*)q, (const uint16_t*)k, (uint16_t*)q_out, (uint16_t*)k_out, rope, L, q ? Hq : 0, k ? Hkv : 0, per, tokens};
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks, (heads + per - 1) / per, B), dim3(64 * WAVES), 0, st, p); };
+  auto with = [&](auto t, auto pairs) {
+    constexpr bool T = decltype(t)::value;
+    constexpr int PAIRS = decltype(pairs)::value;
+    if (d == 64) return go(rotate_kernel<T, 64, PAIRS>);
+    if (d == 96) return go(rotate_kernel<T, 96, PAIRS>);
+    go(rotate_kernel<T, 128, PAIRS>);
   };
-  auto with_type = [&](auto t) { if (vector) with(t, std::true_type{}); else with(t, std::false_type{}); };
+  auto with_type = [&](auto t) {
+    if (rope.interleaved) with(t, std::integral_constant<int, NEIGHBOURS>{});
+    else if (rope.dims % 16 == 0) with(t, std::integral_constant<int, HALVES>{});
+    else with(t, std::integral_constant<int, ODD>{});
+  };
   if (bf16) with_type(std::true_type{}); else with_type(std::false_type{});
   return launch_status("rotate");
 }
