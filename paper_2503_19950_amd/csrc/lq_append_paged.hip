@@ -76,7 +76,7 @@ template <bool BF16, int D, int MODE, int TURN>
 __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPagedParams P, const Rows8<MODE> S) {
   (void)S;
   constexpr int ND = D / 32;
-  const int b = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane / 16;
+  const int b = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), a = lane / 16;
   Row8 row = P.same;
   if constexpr (MODE == ROWS_LISTED) {
     const Row8Ptr r = rows_ptr(P.rows, sizeof(AppendPagedParams));
@@ -95,7 +95,21 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
         P.weights[((((int64_t)row.b * P.Hkv + head0 + x / 32) * P.max_pages) << P.log_p) + 32 * unit + x % 32] = 0.f;
   const int id = P.table[(int64_t)row.b * P.max_pages + (unit >> (P.log_p - 5))];
   if (!is_page(id, P.n_pages)) return;
-  // the first head's rows are under way while the angles are computed
+  // A lane computes the angles of one pair for every fourth token.  What it takes to compute them is loaded first (loads arrive in
+  // order), then the first head's rows, which are under way meanwhile.
+  const int pairs = P.rope.dims / 2;
+  constexpr int TOKENS = 32 / WAVES;
+  double freq = 0.0;
+  int position[TOKENS];
+  if constexpr (TURN) {
+    if (lane < pairs) freq = P.rope.freq[lane];
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j) {
+      const int t = wave + j * WAVES;
+      position[j] = 32 * unit + t;
+      if (P.rope.positions && t >= low && t < high) position[j] = P.rope.positions[(int64_t)b * P.n_max + new0 + t - low];
+    }
+  }
   __amdgpu_buffer_rsrc_t rk;
   u32x4 k[2 * ND], y[ND];
   uint32_t v[ND][8];
@@ -120,12 +134,9 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
   if (h < head1) load(h);
   __shared__ __align__(16) float2 cs[TURN ? 32 * PITCH : 1];
   if constexpr (TURN) {
-    const int pairs = P.rope.dims / 2;
-    for (int x = threadIdx.x; x < (high - low) * pairs; x += 64 * WAVES) {
-      const int t = x / pairs, i = x - t * pairs;
-      const int position = P.rope.positions ? P.rope.positions[(int64_t)b * P.n_max + new0 + t] : 32 * unit + low + t;
-      cs[(low + t) * PITCH + i] = turn_of(P.rope.freq[i], position, P.rope.factor);
-    }
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j)
+      if (lane < pairs) cs[(wave + j * WAVES) * PITCH + lane] = turn_of(freq, position[j], P.rope.factor);
     __syncthreads();
   }
   for (; h < head1; h += WAVES) {

@@ -72,13 +72,24 @@ __global__ void __launch_bounds__(64 * WAVES) rotate_kernel(const RotateParams P
       if (mine && h + j * at_once < head1) x[j] = *reinterpret_cast<const u32x4*>(place(h + j * at_once, false));
     }
   };
+  // A lane computes the angles of one pair for some of the tokens.  What it takes to compute them is loaded
+  // first (loads arrive in order).
+  constexpr int WIDE = D / 2 > 32 ? 64 : 32, EACH = WAVES * 64 / WIDE, MOST = (WAVES * ROWS + EACH - 1) / EACH;
+  const int pair = threadIdx.x % WIDE, s0 = threadIdx.x / WIDE;
+  double freq = 0.0;
+  int position[MOST];
+  if (pair < half) freq = P.rope.freq[pair];
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) {
+    const int s = s0 + i * EACH;
+    position[i] = t0 + s;
+    if (P.rope.positions && s < here) position[i] = P.rope.positions[(int64_t)b * P.L + t0 + s];
+  }
   int h = head0 + row / P.tokens;
   load(h);
-  for (int i = threadIdx.x; i < here * half; i += 64 * WAVES) {
-    const int s = i / half, p = i - s * half;
-    const int position = P.rope.positions ? P.rope.positions[(int64_t)b * P.L + t0 + s] : t0 + s;
-    angles[s * PITCH + p] = turn_of(P.rope.freq[p], position, P.rope.factor);
-  }
+#pragma unroll
+  for (int i = 0; i < MOST; ++i)
+    if (s0 + i * EACH < here && pair < half) angles[(s0 + i * EACH) * PITCH + pair] = turn_of(freq, position[i], P.rope.factor);
   __syncthreads();
   // of the lane's pairs, four or eight: the sine's sign is that of the other half in the result
   float co[8], si[8];
