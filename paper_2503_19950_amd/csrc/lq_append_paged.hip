@@ -200,9 +200,11 @@ hipError_t append_paged(const ShapePaged& s, const AppendPagedParams& p, const R
 
 hipError_t launch_append_paged(const ShapePaged& s, const lq_cache_paged& c, const RopeArg& rope, const void* k_new, const void* v_new,
                                int n_max, int units, const RowArg8& rows, hipStream_t st) {
-  // heads of a workgroup share its angles; fewer where there are few workgroups
-  int heads = s.Hkv;
-  while (heads > WAVES && (int64_t)units * s.B * ((s.Hkv + heads - 1) / heads) < 1024) heads = (heads + 1) / 2;
+  // A head a wavefront: two share the angles, but there are fewer workgroups to fill the GPU (8 rows of up to 8191 tokens x 8 kv heads
+  // 64.8 and 67.0 us; 8 rows of 8192 109.8 and 111.3), which only pays where turning takes longest, halves that are no whole pieces
+  // (136.4 and 125.7).
+  const bool odd = rope.freq && !rope.interleaved && rope.dims % 16;
+  const int heads = odd && s.Hkv > WAVES ? 2 * WAVES : WAVES;
   AppendPagedParams p{(const uint16_t*)k_new, (const uint16_t*)v_new, (uint16_t*)c.k_pages, (uint16_t*)c.v_pages, c.table,
                       s.weighted ? c.weights : nullptr, rope, nullptr, rows.host[0], s.B, s.Hkv, heads, log2_of(s.P), s.n_pages, s.max_pages,
                       n_max};
