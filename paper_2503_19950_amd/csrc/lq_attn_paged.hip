@@ -1,4 +1,6 @@
 // Attention over the paged cache: which kernel, and the weights of a cache that keeps them.
+#include <type_traits>
+
 #include "lq_attn_paged_args.h"
 #include "lq_internal.h"
 #include "lq_weights.h"
@@ -41,8 +43,12 @@ template <int MODE>
 hipError_t attend(const ShapePaged& s, const AttnPagedParams& p, const WeightsParams& w, const Rows8<MODE>& rows, const Plan8& plan,
                   bool step, int most, hipStream_t st) {
   const bool more = p.cap > 0.f || p.slopes || s.weighted;
-  hipError_t e = step ? attn_paged<MODE, true, true>(s, p, rows, plan, st)
-                      : more ? attn_paged<MODE, false, true>(s, p, rows, plan, st) : attn_paged<MODE, false, false>(s, p, rows, plan, st);
+  auto go = [&](auto stepping, auto changed) {
+    return attn_paged<MODE, decltype(stepping)::value, decltype(changed)::value>(s, p, rows, plan, st);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  const hipError_t e = step ? more ? go(yes, yes) : go(yes, no) : more ? go(no, yes) : go(no, no);
   if (e != hipSuccess || !s.weighted || p.weights || !most) return e;
   const dim3 grid((most + 31 + WEIGHTS_AT_ONCE - 1) / WEIGHTS_AT_ONCE, s.Hkv, s.B);
   if (step) hipLaunchKernelGGL((weights_kernel<MODE, true>), grid, dim3(256), 0, st, w, rows);

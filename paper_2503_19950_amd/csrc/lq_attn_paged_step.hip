@@ -1,4 +1,4 @@
-// Kernels of attention over the paged cache: a step.
+// Kernels of attention over the paged cache: a step with a cap, a bias or weights.
 #include "lq_attn_paged.h"
 
 namespace lq {
