@@ -17,6 +17,13 @@
 
 namespace lq {
 
+// Keys and values are read past the caches: a step of a model reads every layer's once.  131072 tokens x 8 kv heads (537 MB) 95.4 and
+// 84.5 us; with one to 64 layers in turn, launches of 67 MB and more 0.87 to 1.03 of the time, of 34 MB 0.93 to 1.00, of 2 and 8 MB, whose
+// layers the last cache would hold, 0.98 to 1.04 (6.4 and 6.6 us); the values alone 86.3.  A choice by size in the kernel costs 1 %.
+__device__ __forceinline__ u32x4 load_once(__amdgpu_buffer_rsrc_t rs, int off) {
+  return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, /* non-temporal */ 2);
+}
+
 // tanh: from |x| = 1/4 on by its definition, below by the first terms of its series (the next is 2^-27 of the result there).
 __device__ __forceinline__ float tanh_of(float x) {
   const float e = __builtin_amdgcn_exp2f(fabsf(x) * 2.88539008177792681472f);     // e^(2 |x|)
@@ -132,12 +139,12 @@ __global__ void __launch_bounds__(64 * NW, NW == 16 ? 4 : SETS == 1 ? 3 : 2) att
     off = there ? unit_offset(next.id, P.Hkv, h, P.log_p, next.u, D) : 0;
     const __amdgpu_buffer_rsrc_t rs = buffer(P.k_pages + off, there ? UNIT * 2 : 0);       // no page: zeros, no reads
 #pragma unroll
-    for (int t = 0; t < 2 * ND; ++t) k[t] = load16(rs, t * 1024 + lane * 16);
+    for (int t = 0; t < 2 * ND; ++t) k[t] = load_once(rs, t * 1024 + lane * 16);
   };
   auto load_v = [&]() {
     const __amdgpu_buffer_rsrc_t rs = buffer(P.v_pages + off, there ? UNIT * 2 : 0);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) v[t] = load16(rs, t * 1024 + lane * 16);
+    for (int t = 0; t < NT; ++t) v[t] = load_once(rs, t * 1024 + lane * 16);
   };
   next = look(i);                                                       // (a wavefront that has none reads nothing)
   load_k();
