@@ -797,7 +797,7 @@ class DeviceCachePaged:
         self.seq_state, self.workspace = buf(self.sizes.seq_state), buf(self.sizes.workspace)
         self.n, self.cur, self.pages = (C.c_int32 * B)(), (C.c_int32 * B)(), (C.c_int32 * (2 * B))()
         self.ids = [[[] for _ in range(B)] for _ in range(2)]     # pages that the table names, by half and row
-        self.free = list(range(cfg.n_pages - 1, -1, -1))
+        self.free, self.uses = list(range(cfg.n_pages - 1, -1, -1)), [0] * cfg.n_pages
         self.c = lq_cache_paged(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.table.data_ptr(),
                                 self.weights.data_ptr() if cfg.weighted else None, *(C.cast(x, _I32P) for x in (self.n, self.cur, self.pages)),
                                 self.seq_state.data_ptr())
@@ -805,30 +805,53 @@ class DeviceCachePaged:
         self._index = self.device.index
         self._cfg, self._c, self._ws = C.byref(cfg), C.byref(self.c), self.workspace.data_ptr()
         self._q_shape, self._token = torch.Size((B, cfg.Hq, cfg.d)), torch.Size((B, cfg.Hkv, 1, cfg.d))
-        self._scores, self._scores_of = None, (0.0, 0, None)
         _on_device(self._index, _init_paged, self._cfg, self._ws)
 
-    # ---- pages
-    def set_pages(self, b, ids, spare=False):
-        """The pages of row b's tokens, in order (`spare`: those that its next eviction moves to).  Pages that were named
-        there before and by no other row go back to the pool, pages named here leave it."""
-        ids = [int(i) for i in ids]
-        if len(ids) > self.cfg.max_pages or any(not 0 <= i < self.cfg.n_pages for i in ids):
-            raise ValueError("set_pages: expected up to %d pages in 0 .. %d" % (self.cfg.max_pages, self.cfg.n_pages - 1))
-        if not spare and len(ids) * self.cfg.page < self.n[b]:
-            raise ValueError("set_pages: row %d holds %d tokens" % (b, self.n[b]))
-        half = self.cur[b] ^ int(bool(spare))
-        before, self.ids[half][b] = self.ids[half][b], ids
-        used = {i for part in self.ids for row in part for i in row}
-        known = set(self.free)
-        self.free = [i for i in self.free if i not in used] + [i for i in dict.fromkeys(before) if i not in used and i not in known]
-        self._name(half, b, 0)
+    def clone(self):
+        """A second cache with its own device buffers and the same contents, pages and counts."""
+        other = DeviceCachePaged(self.cfg, self.device)
+        for name in self.BUFFERS:
+            if getattr(self, name) is not None:
+                getattr(other, name).copy_(getattr(self, name))
+        other.ids, other.uses, other.free = [[list(x) for x in half] for half in self.ids], list(self.uses), list(self.free)
+        other.pages[:] = list(self.pages)
+        other.set_counts(self.counts(), list(self.cur))
+        return other
 
-    def _name(self, half, b, first):
-        ids = self.ids[half][b]
+    # ---- pages
+    def _name(self, half, b, ids, first):
+        """The pages of a row's half are now `ids`, of which those before the first-th were its own."""
+        before, self.ids[half][b] = self.ids[half][b], ids
+        for i in ids[first:]:
+            self.uses[i] += 1
+        for i in before[first:]:
+            self.uses[i] -= 1
+            if not self.uses[i]:
+                self.free.append(i)
         if len(ids) > first:
             self.table[half, b, first:len(ids)] = torch.tensor(ids[first:], dtype=torch.int32)
         self.pages[half * self.cfg.B + b] = len(ids)
+
+    def set_pages(self, b, ids, spare=False):
+        """The pages of row b's tokens, in order (`spare`: those that its next eviction moves to, which nothing else may
+        name).  Pages that were named there before, and by nothing else, go back to the pool."""
+        ids = [int(i) for i in ids]
+        if len(ids) > self.cfg.max_pages or any(not 0 <= i < self.cfg.n_pages for i in ids):
+            raise ValueError("set_pages: expected up to %d pages in 0 .. %d" % (self.cfg.max_pages, self.cfg.n_pages - 1))
+        half = self.cur[b] ^ int(bool(spare))
+        if not spare and len(ids) * self.cfg.page < self.n[b]:
+            raise ValueError("set_pages: row %d holds %d tokens" % (b, self.n[b]))
+        if spare:
+            mine = set(self.ids[half][b])
+            if len(set(ids)) < len(ids) or any(self.uses[i] > (i in mine) for i in ids):
+                raise ValueError("set_pages: a spare page is one that nothing else names")
+        else:
+            spares = {i for row in range(self.cfg.B) for i in self.ids[self.cur[row] ^ 1][row]}
+            if spares & set(ids):
+                raise ValueError("set_pages: a row's spare page is not another's")
+        taken = {i for i in ids if not self.uses[i]}
+        self.free = [i for i in self.free if i not in taken]
+        self._name(half, b, ids, 0)
 
     def reserve(self, counts, spare=False):
         """Pages out of the pool for counts[b] tokens of every row (`spare`: for its next eviction).  LogQuantError
@@ -839,24 +862,25 @@ class DeviceCachePaged:
         more = []
         for b, count in enumerate(counts):
             half = self.cur[b] ^ int(bool(spare))
-            need = -(-int(count) // cfg.page) - len(self.ids[half][b])
+            need = -(-int(count) // cfg.page)
+            if need > cfg.max_pages:
+                raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
+            need -= len(self.ids[half][b])
             if need > 0:
                 more.append((half, b, need))
-            if len(self.ids[half][b]) + max(need, 0) > cfg.max_pages:
-                raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
         if sum(need for _, _, need in more) > len(self.free):
             raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
         for half, b, need in more:
-            first = len(self.ids[half][b])
-            self.ids[half][b] += [self.free.pop() for _ in range(need)]
-            self._name(half, b, first)
+            ids = self.ids[half][b]
+            self._name(half, b, ids + [self.free.pop() for _ in range(need)], len(ids))
 
     def release(self, b, spare=False):
         """Row b gives its pages back and is empty (`spare`: gives back those that it has for its next eviction, or had
         before its last)."""
         if not spare:
             self.n[b] = 0
-        self.set_pages(b, [], spare)
+        half = self.cur[b] ^ int(bool(spare))
+        self._name(half, b, [], 0)
 
     # ---- counts
     def counts(self):
@@ -874,20 +898,18 @@ class DeviceCachePaged:
             if positions is not None:
                 raise ValueError("positions without a rope")
             return None, None
-        if rope.device != self.device:
+        if rope.index != self._index:
             raise ValueError("rope: expected it on %s" % self.device)
         if positions is None:
             return rope._c, None
-        shape = torch.Size((self.cfg.B,) if n == 1 and positions.dim() == 1 else (self.cfg.B, n))
+        shape = (self.cfg.B,) if n == 1 and positions.dim() == 1 else (self.cfg.B, n)
         return rope._c, _tensor("positions", positions, shape, torch.int32, self.device)
 
     def _how(self, softcap, window, slopes):
         if not softcap and not window and slopes is None:
             return None
-        at = None if slopes is None else _tensor("slopes", slopes, torch.Size((self.cfg.Hq,)), torch.float32, self.device)
-        if (softcap, window, at) != self._scores_of or self._scores is None:
-            self._scores, self._scores_of = lq_scores(softcap, window, at), (softcap, window, at)
-        return C.byref(self._scores)
+        at = None if slopes is None else _tensor("slopes", slopes, (self.cfg.Hq,), torch.float32, self.device)
+        return C.byref(lq_scores(softcap, window, at))
 
     def append(self, k_new, v_new, n_new=None, rope=None, positions=None):
         """k_new, v_new: [B][Hkv][n][d]; n_new: tokens that each row takes of them, 0..n (None: all).  With a rope, keys are
@@ -929,5 +951,9 @@ class DeviceCachePaged:
         keep = [int(keep)] * self.cfg.B if isinstance(keep, int) else [int(x) for x in keep]
         if len(keep) != self.cfg.B:
             raise ValueError("keep: expected %d counts" % self.cfg.B)
+        for b, (n, x) in enumerate(zip(self.n, keep)):
+            spare = self.ids[self.cur[b] ^ 1][b]
+            if n > x and any(self.uses[i] > 1 for i in spare):           # left by an eviction, but another row's as well
+                self.release(b, spare=True)
         self.reserve([x if n > x else 0 for n, x in zip(self.n, keep)], spare=True)
         _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)

@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(256) move_kernel(const EvictParams P, const Ro
   auto store_k = [&]() {
 #pragma unroll
     for (int x = 0; x < 2 * ND; ++x)
-      if (16 * (x / ND) + lane % 16 < here) *reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8) = k[x];
+      if (16 * (x / ND) + lane % 16 < here) __builtin_nontemporal_store(k[x], reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8));
   };
   uint16_t* mine = stage[wave];
   if (__popc(starts) <= DENSE) {
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(256) move_kernel(const EvictParams P, const Ro
       uint16_t* to = P.v_pages + off + t * 512 + lane * 8;
       const u32x4 y = *reinterpret_cast<const u32x4*>(mine + t * 512 + lane * 8);
       if (here == 32) {
-        *reinterpret_cast<u32x4*>(to) = y;
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(to));
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)

@@ -99,7 +99,8 @@ def test_step_is_rotate_append_attend(dims, interleaved, positions, dtype):
         model.check_output(out, tq[:, :, 0], window=i * 20)
 
 
-@pytest.mark.parametrize("heads,lengths", [((24, 1), [40, 3000]), ((17, 1), [9000]), ((16, 16), [100] * 3), ((32, 8), [4000] * 9), ((4, 4), [1 + 97 * b % 900 for b in range(70)])])
+@pytest.mark.parametrize("heads,lengths", [((24, 1), [40, 3000]), ((17, 1), [9000]), ((16, 16), [100] * 3), ((32, 8), [4000] * 9), ((4, 4), [1 + 97 * b % 900 for b in range(70)]),
+                                           ((2, 1), [37 * b % 200 for b in range(260)])])
 def test_steps_of_other_shapes(heads, lengths):
     Hq, Hkv = heads
     dtype, d, page, B = "bf16", 128, 32, len(lengths)

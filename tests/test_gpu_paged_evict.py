@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 def _filled(seed, lengths, Hkv, d, page, dtype, values, n_pages=None):
     """A weighted cache whose weights are drawn from `values`."""
     B = len(lengths)
-    cache = U.make(B, Hkv, Hkv, d, page, dtype, -(-max(lengths) // page) + 1, weighted=True, seed=seed, n_pages=n_pages)
+    cache = U.make(B, Hkv, Hkv, d, page, dtype, -(-max(lengths) // page) + 2, weighted=True, seed=seed, n_pages=n_pages)
     cache.reserve(lengths)
     K, V = U.rows(seed, B, Hkv, max(lengths), d, dtype=dtype), U.rows(seed + 1, B, Hkv, max(lengths), d, dtype=dtype)
     cache.append(K.to(U.DEVICE), V.to(U.DEVICE), lengths)
@@ -70,12 +70,76 @@ def test_evict(case, values):
         assert torch.equal(now[1, b, :, tail:], other[1, b, :, tail:])
 
 
-def test_a_long_row():
-    cache, model = _filled(3, [70001], 1, 64, 128, "bf16", VALUES["spread"])
+@pytest.mark.parametrize("values", VALUES)
+@pytest.mark.parametrize("lengths,keep,recent,d", [([70001], 33333, 4096, 64), ([16385, 16384, 40, 20001], [300, 9000, 40, 20000], 0, 128),
+                                                   ([18500, 100], [2048, 50], 50, 96)])
+def test_long_rows(lengths, keep, recent, d, values):
+    cache, model = _filled(3, lengths, 1, d, 128, "bf16", VALUES[values])
     before = U.pools(cache)
-    cache.evict(33333, 4096)
-    model.evict(33333, 4096)
+    cache.evict(keep, recent)
+    model.evict(keep, recent)
     _check(cache, model, before)
+
+
+@pytest.mark.parametrize("lengths,keep,recent,d,page", [([6000, 3000], 200, 7, 96, 64), ([9000], 500, 3, 128, 32), ([4000, 4100], [64, 600], 0, 64, 128)])
+def test_few_stay_of_many(lengths, keep, recent, d, page):
+    """Tokens of a unit that come from many others."""
+    cache, model = _filled(5, lengths, 2, d, page, "f16", VALUES["spread"])
+    before = U.pools(cache)
+    cache.evict(keep, recent)
+    model.evict(keep, recent)
+    _check(cache, model, before)
+
+
+def test_replays_of_a_recorded_eviction():
+    """Replayed, it moves the same tokens' places again, by the weights as they are then."""
+    lengths, keep, recent = [17000, 300, 90], 200, 20
+    cache, model = _filled(13, lengths, 1, 64, 32, "f16", VALUES["spread"])
+    cache.reserve([200, 200, 0], spare=True)
+    before = U.pools(cache)
+    K, V = [x.copy() for x in model.K], [x.copy() for x in model.V]
+    halves = list(cache.cur)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        cache.evict(keep, recent)                                        # (code is loaded before the recording)
+    stream.synchronize()
+    cache.set_counts(lengths, halves)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        cache.evict(keep, recent)
+    for i in range(3):
+        r = np.random.RandomState(50 + i)
+        model.K, model.V = [x.copy() for x in K], [x.copy() for x in V]
+        for b, n in enumerate(lengths):
+            w = VALUES["few" if i else "spread"](r, (1, n)).astype(np.float32)
+            cache.weights[0, b, :, :n] = torch.from_numpy(w).to(U.DEVICE)
+            model.w[b] = w.astype(np.float64)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        model.evict(keep, recent)
+        _check(cache, model, before)
+        q = U.rows(i, 3, 1, 64, dtype="f16")
+        model.check_output(cache.decode_attn(q.to(U.DEVICE)), q)         # (adds to the weights of the evicted rows' halves)
+        model.w = [x.copy() for x in model.w]
+
+
+def test_a_page_that_a_row_names_twice():
+    cache, model = _filled(9, [64], 1, 64, 32, "f16", VALUES["spread"])
+    cache.set_pages(0, cache.ids[0][0] + cache.ids[0][0])
+    cache.n[0] = 128
+    model.K[0], model.V[0] = (np.concatenate([x[0], x[0]], 1) for x in (model.K, model.V))
+    w = np.float32(np.random.RandomState(1).rand(1, 128))
+    cache.weights[0, 0, :, :128] = torch.from_numpy(w).to(U.DEVICE)
+    for keep, recent in ((100, 50), (70, 0)):
+        model.w[0] = w.astype(np.float64)
+        one, two = cache.clone(), U.Model(cache, "f16")
+        two.K, two.V, two.w = [x.copy() for x in model.K], [x.copy() for x in model.V], [x.copy() for x in model.w]
+        before = U.pools(one)
+        one.evict(keep, recent)
+        two.evict(keep, recent)
+        _check(one, two, before)
 
 
 def test_tokens_without_a_page_become_zeros():

@@ -111,6 +111,70 @@ def test_rows_that_share_a_prefix():
     assert sorted(cache.free) == list(range(12)) and cache.counts() == [0, 0, 0]
 
 
+def test_pages_have_one_owner_or_are_read_only():
+    cache = U.make(3, 1, 1, 64, 32, "f16", 4, n_pages=14, weighted=True)
+    cache.reserve([64, 64, 32])
+    a, b = list(cache.ids[0][0]), list(cache.ids[0][1])
+    with pytest.raises(ValueError):
+        cache.set_pages(1, a[:1], spare=True)                            # another row reads it
+    with pytest.raises(ValueError):
+        cache.set_pages(1, [cache.free[0], cache.free[0]], spare=True)   # twice
+    cache.reserve([32, 0, 0], spare=True)
+    with pytest.raises(ValueError):
+        cache.set_pages(2, cache.ids[1][0])                              # another row's spare one
+    cache.set_pages(2, a + a[:1])                                        # shared, one twice
+    assert [cache.uses[i] for i in a] == [3, 2] and len(cache.free) == 14 - 4 - 1
+    cache.set_pages(2, [])
+    assert [cache.uses[i] for i in a + b] == [1] * 4
+    # the pages that an eviction leaves are not written by the next one while another row reads them
+    K = U.rows(1, 3, 1, 64, 64, dtype="f16").to(U.DEVICE)
+    cache.append(K, K, [64, 64, 0])
+    cache.set_pages(2, a)
+    cache.n[2] = 64
+    before = cache.clone()
+    assert before.free == cache.free and before.ids == cache.ids and before.counts() == cache.counts()
+    cache.evict([32, 64, 64], 32)
+    cache.reserve([60, 64, 64])
+    cache.append(K, K, [28, 0, 0])
+    cache.evict([32, 64, 64], 32)
+    assert not set(a) & set(cache.ids[0][0]) and [cache.uses[i] for i in a] == [1, 1]
+    q = U.rows(2, 3, 1, 64, dtype="f16").to(U.DEVICE)
+    assert torch.equal(cache.decode_attn(q)[1:], before.decode_attn(q)[1:])
+
+
+def test_places_beyond_four_gigabytes():
+    """A pool of 6 GB a tensor: a row whose pages lie at its end, one at its start."""
+    Hkv, d, page, dtype = 8, 128, 128, "bf16"
+    n_pages = 6 * 10 ** 9 // (Hkv * d * page * 2)
+    cache = binding.DeviceCachePaged(binding.make_config_paged(2, 16, Hkv, d, page, dtype, n_pages, 3, True), U.DEVICE)
+    cache.set_pages(0, [n_pages - 1, n_pages - 3, n_pages // 2])
+    cache.set_pages(1, [0, 2, 1])
+    K, V = U.rows(1, 2, Hkv, 300, d, dtype=dtype), U.rows(2, 2, Hkv, 300, d, dtype=dtype)
+    model = U.Model(cache, dtype)
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE))
+    model.append(K, V)
+    q = U.rows(3, 2, 16, d, dtype=dtype)
+    k, v = U.rows(4, 2, Hkv, 1, d, dtype=dtype), U.rows(5, 2, Hkv, 1, d, dtype=dtype)
+    out = cache.decode_step(k.to(U.DEVICE), v.to(U.DEVICE), q.to(U.DEVICE))
+    model.append(k, v)
+    model.check_output(out, q, weights=U.live_weights(cache))
+    pools = {w: getattr(cache, w + "_pages").view(torch.bfloat16) for w in "kv"}
+
+    def held(w, b, h):
+        return U.f64(pools[w][torch.from_numpy(U.addresses(cache, w, b, h, cache.n[b])).to(U.DEVICE)])
+
+    def check():
+        for b in range(2):
+            for h in range(Hkv):
+                assert np.array_equal(held("k", b, h), model.K[b][h]) and np.array_equal(held("v", b, h), model.V[b][h])
+    check()
+    cache.set_pages(0, [n_pages - 7, n_pages - 2], spare=True)
+    cache.set_pages(1, [n_pages - 8, 5], spare=True)
+    cache.evict(200, 20)
+    model.evict(200, 20)
+    check()
+
+
 def test_the_pool_runs_out():
     cache = U.make(2, 1, 1, 64, 32, "f16", 8, n_pages=5)
     cache.reserve([64, 33])
