@@ -797,7 +797,7 @@ class DeviceCachePaged:
         self.seq_state, self.workspace = buf(self.sizes.seq_state), buf(self.sizes.workspace)
         self.n, self.cur, self.pages = (C.c_int32 * B)(), (C.c_int32 * B)(), (C.c_int32 * (2 * B))()
         self.ids = [[[] for _ in range(B)] for _ in range(2)]     # pages that the table names, by half and row
-        self.free, self.uses = list(range(cfg.n_pages - 1, -1, -1)), [0] * cfg.n_pages
+        self.free, self.uses = dict.fromkeys(range(cfg.n_pages - 1, -1, -1)), [0] * cfg.n_pages
         self.c = lq_cache_paged(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.table.data_ptr(),
                                 self.weights.data_ptr() if cfg.weighted else None, *(C.cast(x, _I32P) for x in (self.n, self.cur, self.pages)),
                                 self.seq_state.data_ptr())
@@ -813,24 +813,35 @@ class DeviceCachePaged:
         for name in self.BUFFERS:
             if getattr(self, name) is not None:
                 getattr(other, name).copy_(getattr(self, name))
-        other.ids, other.uses, other.free = [[list(x) for x in half] for half in self.ids], list(self.uses), list(self.free)
+        other.ids, other.uses, other.free = [[list(x) for x in half] for half in self.ids], list(self.uses), dict(self.free)
         other.pages[:] = list(self.pages)
         other.set_counts(self.counts(), list(self.cur))
         return other
 
     # ---- pages
     def _name(self, half, b, ids, first):
-        """The pages of a row's half are now `ids`, of which those before the first-th were its own."""
+        """The pages of a row's half are now `ids`, of which those before the first-th were its own.  -> what that makes of
+        the table: places and pages."""
         before, self.ids[half][b] = self.ids[half][b], ids
+        uses = self.uses
         for i in ids[first:]:
-            self.uses[i] += 1
+            uses[i] += 1
+            if uses[i] == 1:
+                self.free.pop(i, None)
         for i in before[first:]:
-            self.uses[i] -= 1
-            if not self.uses[i]:
-                self.free.append(i)
-        if len(ids) > first:
-            self.table[half, b, first:len(ids)] = torch.tensor(ids[first:], dtype=torch.int32)
-        self.pages[half * self.cfg.B + b] = len(ids)
+            uses[i] -= 1
+            if not uses[i]:
+                self.free[i] = None
+        row = half * self.cfg.B + b
+        self.pages[row] = len(ids)
+        at = row * self.cfg.max_pages
+        return range(at + first, at + len(ids)), ids[first:]
+
+    def _upload(self, names):
+        places = [i for at, _ in names for i in at]
+        if places:
+            both = torch.tensor([places, [i for _, ids in names for i in ids]]).to(self.device)
+            self.table.view(-1)[both[0]] = both[1].int()
 
     def set_pages(self, b, ids, spare=False):
         """The pages of row b's tokens, in order (`spare`: those that its next eviction moves to, which nothing else may
@@ -846,12 +857,10 @@ class DeviceCachePaged:
             if len(set(ids)) < len(ids) or any(self.uses[i] > (i in mine) for i in ids):
                 raise ValueError("set_pages: a spare page is one that nothing else names")
         else:
-            spares = {i for row in range(self.cfg.B) for i in self.ids[self.cur[row] ^ 1][row]}
-            if spares & set(ids):
+            named = set(ids)
+            if any(i in named for row in range(self.cfg.B) for i in self.ids[self.cur[row] ^ 1][row]):
                 raise ValueError("set_pages: a row's spare page is not another's")
-        taken = {i for i in ids if not self.uses[i]}
-        self.free = [i for i in self.free if i not in taken]
-        self._name(half, b, ids, 0)
+        self._upload([self._name(half, b, ids, 0)])
 
     def reserve(self, counts, spare=False):
         """Pages out of the pool for counts[b] tokens of every row (`spare`: for its next eviction).  LogQuantError
@@ -870,9 +879,11 @@ class DeviceCachePaged:
                 more.append((half, b, need))
         if sum(need for _, _, need in more) > len(self.free):
             raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
+        names = []
         for half, b, need in more:
             ids = self.ids[half][b]
-            self._name(half, b, ids + [self.free.pop() for _ in range(need)], len(ids))
+            names.append(self._name(half, b, ids + [self.free.popitem()[0] for _ in range(need)], len(ids)))
+        self._upload(names)
 
     def release(self, b, spare=False):
         """Row b gives its pages back and is empty (`spare`: gives back those that it has for its next eviction, or had

@@ -78,7 +78,9 @@ def make(B, Hq, Hkv, d, page, dtype, max_pages, n_pages=None, weighted=False, se
     """A poisoned cache whose free pages are in a scattered order."""
     n_pages = n_pages or B * max_pages * (2 if weighted else 1) + 3
     cache = binding.DeviceCachePaged(binding.make_config_paged(B, Hq, Hkv, d, page, dtype, n_pages, max_pages, weighted), DEVICE, poison=True)
-    np.random.RandomState(seed).shuffle(cache.free)
+    order = list(cache.free)
+    np.random.RandomState(seed).shuffle(order)
+    cache.free = dict.fromkeys(order)
     return cache
 
 

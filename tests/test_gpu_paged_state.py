@@ -118,7 +118,7 @@ def test_pages_have_one_owner_or_are_read_only():
     with pytest.raises(ValueError):
         cache.set_pages(1, a[:1], spare=True)                            # another row reads it
     with pytest.raises(ValueError):
-        cache.set_pages(1, [cache.free[0], cache.free[0]], spare=True)   # twice
+        cache.set_pages(1, [next(iter(cache.free))] * 2, spare=True)   # twice
     cache.reserve([32, 0, 0], spare=True)
     with pytest.raises(ValueError):
         cache.set_pages(2, cache.ids[1][0])                              # another row's spare one
