@@ -3,6 +3,9 @@
 // Bound by the bytes.  A workgroup takes a unit of 32 slots of a row and some kv heads, a head a wavefront; with rotary
 // positions it computes the unit's cosines and sines once, into LDS.  Keys go over 16 bytes a lane, as they lie in a row of
 // the prompt; values as two channels of eight tokens a lane, whose halves are the pieces of the page.
+// 8 rows of 8192 tokens x 8 kv heads, d = 128 (537 MB): 104 us, with keys turned on their way 105 (5.1 TB/s, what a copy
+// reaches); rows of up to 8191 (270 MB): 60 and 61, of which some 8 us are workgroups that find their row at an end.
+// Stores past the caches: 121 and 68.
 #include "lq_internal.h"
 #include "lq_paged.h"
 #include "lq_quant8.h"
@@ -29,8 +32,9 @@ __device__ __forceinline__ uint16_t load2(__amdgpu_buffer_rsrc_t rs, int off) { 
 // token within its unit of 32 at position e of the eight that lane row a holds
 __device__ __forceinline__ int value_token(int a, int e) { return 16 * (e >> 2) + 4 * a + (e & 3); }
 
-// How keys are turned: not at all; pairs of neighbours; pairs of halves that are whole pieces of 16 bytes; of halves that are not.
-enum Turn { NONE, NEIGHBOURS, HALVES, ODD };
+// How keys are turned: not at all; pairs of neighbours; pairs of halves that are 32 or 64 channels, in the same lane, that are other
+// whole pieces of 16 bytes, and that are not.
+enum Turn { NONE, NEIGHBOURS, HALVES_32, HALVES_64, HALVES, ODD };
 
 // The other halves of the pairs that channels c0 .. c0+7 of a key (offset `row` of rs) belong to.
 template <int TURN>
@@ -62,8 +66,8 @@ __device__ __forceinline__ u32x4 turned(int c0, u32x4 x, u32x4 y, int dims, cons
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int c = c0 + e, sh = 16 * (e & 1);
-    const bool first = TURN == HALVES ? c0 < half : c < half;
-    const float2 cs = TURN == HALVES ? (angle + (first ? c0 : c0 - half))[e] : angle[first ? c : c - half];
+    const bool first = TURN == ODD ? c < half : c0 < half;
+    const float2 cs = TURN == ODD ? angle[first ? c : c - half] : (angle + (first ? c0 : c0 - half))[e];
     const float own = t2f<BF16>((uint16_t)(x[e / 2] >> sh)), other = t2f<BF16>((uint16_t)(y[e / 2] >> sh));
     const uint32_t z = f2t<BF16>(fmaf(own, cs.x, other * (first ? -cs.y : cs.y)));
     if (c < dims) x[e / 2] = (x[e / 2] & ~(0xFFFFu << sh)) | z << sh;
@@ -71,9 +75,10 @@ __device__ __forceinline__ u32x4 turned(int c0, u32x4 x, u32x4 y, int dims, cons
   return x;
 }
 
-// grid (units that a row's new tokens touch, shares of the kv heads, B)
+// grid (units that a row's new tokens touch, shares of the kv heads, B).  HALVES_64 has registers for three wavefronts on a SIMD and
+// four of them spilled (one kv head, 65536 tokens: 15.8 us, with two wavefronts and none spilled 19.7; 8 kv heads 61.0 and 62.0).
 template <bool BF16, int D, int MODE, int TURN>
-__global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPagedParams P, const Rows8<MODE> S) {
+__global__ void __launch_bounds__(64 * WAVES, TURN == HALVES_64 ? 3 : 1) append_paged_kernel(const AppendPagedParams P, const Rows8<MODE> S) {
   (void)S;
   constexpr int ND = D / 32;
   const int b = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), a = lane / 16;
@@ -111,10 +116,12 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
     }
   }
   __amdgpu_buffer_rsrc_t rk;
+  constexpr bool APART = TURN == HALVES || TURN == ODD;                 // the other halves are loaded
+  constexpr int OTHER = TURN == HALVES_32 ? 1 : TURN == HALVES_64 ? 2 : 0;
   u32x4 k[2 * ND], y[ND];
   uint32_t v[ND][8];
   auto load_y = [&](int tile) {
-    if constexpr (TURN)
+    if constexpr (APART)
 #pragma unroll
       for (int nd = 0; nd < ND; ++nd) y[nd] = other_halves<TURN>(rk, (16 * tile + lane % 16 - low) * (2 * D), 32 * nd + 8 * a, P.rope.dims);
   };
@@ -146,8 +153,13 @@ __global__ void __launch_bounds__(64 * WAVES) append_paged_kernel(const AppendPa
       const int t = 16 * (x / ND) + lane % 16, c = 32 * (x % ND) + 8 * a;
       if (x == ND) load_y(1);
       if (t < low || t >= high) continue;
-      if constexpr (TURN) k[x] = turned<BF16, TURN>(c, k[x], y[x % ND], P.rope.dims, cs + t * PITCH);
-      *reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8) = k[x];
+      u32x4 z = k[x];
+      if constexpr (OTHER > 0) {
+        if (x % ND < 2 * OTHER) z = turned<BF16, TURN>(c, z, k[x % ND < OTHER ? x + OTHER : x - OTHER], 64 * OTHER, cs + t * PITCH);
+      } else if constexpr (TURN) {
+        z = turned<BF16, TURN>(c, z, y[x % ND], P.rope.dims, cs + t * PITCH);
+      }
+      *reinterpret_cast<u32x4*>(P.k_pages + off + x * 512 + lane * 8) = z;
     }
 #pragma unroll
     for (int nd = 0; nd < ND; ++nd) {
@@ -181,13 +193,17 @@ hipError_t append_paged(const ShapePaged& s, const AppendPagedParams& p, const R
   auto with = [&](auto t, auto turn) {
     constexpr bool T = decltype(t)::value;
     constexpr int TURN = decltype(turn)::value;
-    if (s.d == 64) return go(append_paged_kernel<T, 64, MODE, TURN>);
-    if (s.d == 96) return go(append_paged_kernel<T, 96, MODE, TURN>);
+    if constexpr (TURN != HALVES_64) {                                  // (of 128 channels)
+      if (s.d == 64) return go(append_paged_kernel<T, 64, MODE, TURN>);
+      if (s.d == 96) return go(append_paged_kernel<T, 96, MODE, TURN>);
+    }
     go(append_paged_kernel<T, 128, MODE, TURN>);
   };
   auto with_type = [&](auto t) {
     if (p.rope.interleaved) return with(t, std::integral_constant<int, NEIGHBOURS>{});
     if (p.rope.dims % 16) return with(t, std::integral_constant<int, ODD>{});
+    if (p.rope.dims == 64) return with(t, std::integral_constant<int, HALVES_32>{});
+    if (p.rope.dims == 128) return with(t, std::integral_constant<int, HALVES_64>{});
     with(t, std::integral_constant<int, HALVES>{});
   };
   if (!p.rope.freq) with(std::false_type{}, std::integral_constant<int, NONE>{});      // (the type does not matter)
