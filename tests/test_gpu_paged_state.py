@@ -24,10 +24,13 @@ def test_append_in_pieces(d, page, dtype):
         U.check_rows(cache, model, before)
 
 
-@pytest.mark.parametrize("dims,interleaved", [(128, False), (64, True), (48, False), (10, False), (10, True), (126, False)])
-def test_keys_turned_on_their_way_are_keys_turned_before(dims, interleaved):
-    B, Hkv, d, page, dtype = 2, 3, 128, 64, "bf16"
-    cache = U.make(B, 3, Hkv, d, page, dtype, 3)
+@pytest.mark.parametrize("d,dims,interleaved", [(128, 128, False), (128, 64, True), (128, 64, False), (128, 48, False), (128, 10, False),
+                                                (128, 10, True), (128, 126, False), (96, 96, False), (96, 64, False), (96, 2, False),
+                                                (64, 64, False), (64, 32, False), (64, 64, True), (64, 22, False)])
+@pytest.mark.parametrize("Hkv", [1, 5, 9])
+def test_keys_turned_on_their_way_are_keys_turned_before(d, dims, interleaved, Hkv):
+    B, page, dtype = 2, 64, "bf16" if Hkv == 5 else "f16"
+    cache = U.make(B, Hkv, Hkv, d, page, dtype, 3)
     model, before = U.Model(cache, dtype), U.pools(cache)
     cache.reserve([150, 150])
     rope = binding.Rope(binding.logquant_rope_frequencies(dims), interleaved, 0.75, U.DEVICE)
