@@ -303,8 +303,10 @@ __global__ void __launch_bounds__(256) count_kernel(const EvictParams P, const R
 // Rows to their new places: a wavefront a unit of 32 slots.  grid (units / 4, Hkv, rows)
 // Keys are pieces of 16 bytes of a token, gathered.  A piece of values holds eight tokens: units that the tokens come from are read
 // whole, 16 bytes a lane, and what stays of them is put in its place in LDS, two bytes at a time.  Where the tokens of a unit come
-// from more than DENSE others (few stay of many), they are gathered from memory two bytes at a time instead.
-constexpr int DENSE = 8;
+// from more than DENSE others (few stay of many), they are gathered from memory two bytes at a time instead: 8 rows of 16384 tokens x 8
+// kv heads, of which a half, a quarter, a sixth and an eighth stay, 229, 165, 145 and 111 us gathered, 182, 148, 136 and 122 read whole,
+// 181, 151, 145 and 114 by this rule (149 and 119 of a quarter and an eighth with 8 units, 158 and 112 with 6).
+constexpr int DENSE = 7;
 template <int D>
 __global__ void __launch_bounds__(256) move_kernel(const EvictParams P, const Rows8<ROWS_LISTED> S) {
   (void)S;

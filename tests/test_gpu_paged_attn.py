@@ -144,7 +144,7 @@ def test_weights_add_up(how, heads, dtype):
 @pytest.mark.parametrize("lengths,heads,d", [([500] * 40, (32, 8), 64), ([4096 - 61 * b % 3000 for b in range(36)], (32, 8), 128),
                                              ([1 + 37 * b % 700 for b in range(40)], (40, 8), 96), ([3000 - 90 * b for b in range(20)], (64, 16), 64),
                                              ([200] * 33, (8, 8), 96), ([700] * 9, (68, 2), 64), ([9000, 50], (4, 2), 64),
-                                             ([4500] * 40, (32, 8), 64)])
+                                             ([4500] * 40, (32, 8), 64), ([8000 - 100 * b for b in range(36)], (32, 8), 64)])
 @pytest.mark.parametrize("window", [0, 90])
 def test_weights_by_every_route(lengths, heads, d, window):
     Hq, Hkv = heads
@@ -171,6 +171,25 @@ def test_weights_by_every_route(lengths, heads, d, window):
     for b in range(B):
         w = cache.weights[0, b, :, :cache.n[b]].double().sum(-1)
         assert (w - 2 * Hq / Hkv).abs().max() < 2.0 ** -17 * Hq / Hkv
+
+
+def test_a_step_without_a_page_for_its_token():
+    """Nothing is stored, and nothing but the tokens that have a page gets weight."""
+    dtype = "bf16"
+    cache, model = _filled(37, [64, 70], 4, 2, 96, 32, dtype, weighted=True, more=30)
+    cache.table[0, 0, 2] = -1                                            # row 0: of the new token alone
+    cache.table[0, 1, 2] = cache.cfg.n_pages                             # row 1: of the six before it as well
+    before = U.pools(cache)
+    K, V, q = U.rows(1, 2, 2, 1, 96, dtype=dtype), U.rows(2, 2, 2, 1, 96, dtype=dtype), U.rows(3, 2, 4, 96, dtype=dtype)
+    rope = binding.Rope(binding.logquant_rope_frequencies(96), device=U.DEVICE)
+    out = cache.decode_step(K.to(U.DEVICE), V.to(U.DEVICE), q.to(U.DEVICE), rope=rope)
+    assert cache.counts() == [65, 71] and all(np.array_equal(U.pools(cache)[w], before[w]) for w in "kv")
+    w = U.live_weights(cache)
+    assert (w[0, :, 64] == 0).all() and (w[1, :, 64:71] == 0).all()
+    model.K, model.V, model.w = ([x[:, :64] for x in t] for t in (model.K, model.V, model.w))
+    places = torch.tensor([64, 70], dtype=torch.int32, device=U.DEVICE)
+    tq = binding.rotate(rope, places, q.to(U.DEVICE))[0].cpu()
+    model.check_output(out, tq, weights=w)
 
 
 def test_a_cache_without_pages_of_some_rows_weighs_nothing():
