@@ -798,6 +798,7 @@ class DeviceCachePaged:
         self.n, self.cur, self.pages = (C.c_int32 * B)(), (C.c_int32 * B)(), (C.c_int32 * (2 * B))()
         self.ids = [[[] for _ in range(B)] for _ in range(2)]     # pages that the table names, by half and row
         self.free, self.uses = dict.fromkeys(range(cfg.n_pages - 1, -1, -1)), [0] * cfg.n_pages
+        self.shared = 0                                           # pages that are named more than once
         self.c = lq_cache_paged(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.table.data_ptr(),
                                 self.weights.data_ptr() if cfg.weighted else None, *(C.cast(x, _I32P) for x in (self.n, self.cur, self.pages)),
                                 self.seq_state.data_ptr())
@@ -814,6 +815,7 @@ class DeviceCachePaged:
             if getattr(self, name) is not None:
                 getattr(other, name).copy_(getattr(self, name))
         other.ids, other.uses, other.free = [[list(x) for x in half] for half in self.ids], list(self.uses), dict(self.free)
+        other.shared = self.shared
         other.pages[:] = list(self.pages)
         other.set_counts(self.counts(), list(self.cur))
         return other
@@ -828,10 +830,14 @@ class DeviceCachePaged:
             uses[i] += 1
             if uses[i] == 1:
                 self.free.pop(i, None)
+            elif uses[i] == 2:
+                self.shared += 1
         for i in before[first:]:
             uses[i] -= 1
             if not uses[i]:
                 self.free[i] = None
+            elif uses[i] == 1:
+                self.shared -= 1
         row = half * self.cfg.B + b
         self.pages[row] = len(ids)
         at = row * self.cfg.max_pages
@@ -962,9 +968,9 @@ class DeviceCachePaged:
         keep = [int(keep)] * self.cfg.B if isinstance(keep, int) else [int(x) for x in keep]
         if len(keep) != self.cfg.B:
             raise ValueError("keep: expected %d counts" % self.cfg.B)
-        for b, (n, x) in enumerate(zip(self.n, keep)):
-            spare = self.ids[self.cur[b] ^ 1][b]
-            if n > x and any(self.uses[i] > 1 for i in spare):           # left by an eviction, but another row's as well
-                self.release(b, spare=True)
-        self.reserve([x if n > x else 0 for n, x in zip(self.n, keep)], spare=True)
+        if any(n > x for n, x in zip(self.n, keep)):
+            for b, (n, x) in enumerate(zip(self.n, keep) if self.shared else ()):
+                if n > x and any(self.uses[i] > 1 for i in self.ids[self.cur[b] ^ 1][b]):   # left by an eviction, but another row's as well
+                    self.release(b, spare=True)
+            self.reserve([x if n > x else 0 for n, x in zip(self.n, keep)], spare=True)
         _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)

@@ -126,9 +126,9 @@ def test_pages_have_one_owner_or_are_read_only():
     with pytest.raises(ValueError):
         cache.set_pages(2, cache.ids[1][0])                              # another row's spare one
     cache.set_pages(2, a + a[:1])                                        # shared, one twice
-    assert [cache.uses[i] for i in a] == [3, 2] and len(cache.free) == 14 - 4 - 1
+    assert [cache.uses[i] for i in a] == [3, 2] and len(cache.free) == 14 - 4 - 1 and cache.shared == 2
     cache.set_pages(2, [])
-    assert [cache.uses[i] for i in a + b] == [1] * 4
+    assert [cache.uses[i] for i in a + b] == [1] * 4 and cache.shared == 0
     # the pages that an eviction leaves are not written by the next one while another row reads them
     K = U.rows(1, 3, 1, 64, 64, dtype="f16").to(U.DEVICE)
     cache.append(K, K, [64, 64, 0])
