@@ -843,6 +843,12 @@ class DeviceCachePaged:
         at = row * self.cfg.max_pages
         return range(at + first, at + len(ids)), ids[first:]
 
+    def _no_recording(self, call):
+        """Pages are named from the host, which a graph cannot record."""
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():
+                raise LogQuantError(LQ_ERR_STATE, call)
+
     def _upload(self, names):
         places = [i for at, _ in names for i in at]
         if places:
@@ -852,6 +858,7 @@ class DeviceCachePaged:
     def set_pages(self, b, ids, spare=False):
         """The pages of row b's tokens, in order (`spare`: those that its next eviction moves to, which nothing else may
         name).  Pages that were named there before, and by nothing else, go back to the pool."""
+        self._no_recording("set_pages")
         ids = [int(i) for i in ids]
         if len(ids) > self.cfg.max_pages or any(not 0 <= i < self.cfg.n_pages for i in ids):
             raise ValueError("set_pages: expected up to %d pages in 0 .. %d" % (self.cfg.max_pages, self.cfg.n_pages - 1))
@@ -870,7 +877,8 @@ class DeviceCachePaged:
 
     def reserve(self, counts, spare=False):
         """Pages out of the pool for counts[b] tokens of every row (`spare`: for its next eviction).  LogQuantError
-        (LQ_ERR_CAPACITY) if the pool or a row's table has too few; nothing is taken then."""
+        (LQ_ERR_CAPACITY) if the pool or a row's table has too few, or (LQ_ERR_STATE) if any are to be taken while a graph is
+        recorded; nothing is taken then."""
         cfg = self.cfg
         if len(counts) != cfg.B:
             raise ValueError("reserve: expected %d counts" % cfg.B)
@@ -885,6 +893,9 @@ class DeviceCachePaged:
                 more.append((half, b, need))
         if sum(need for _, _, need in more) > len(self.free):
             raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
+        if not more:
+            return
+        self._no_recording("reserve")
         names = []
         for half, b, need in more:
             ids = self.ids[half][b]

@@ -234,3 +234,31 @@ def test_tensors_that_are_refused():
     with pytest.raises(binding.LogQuantError):
         cache.decode_attn(q, window=-1)
     assert cache.counts() == [0, 0]
+
+
+def test_pages_are_not_named_in_a_recording():
+    """A graph cannot record what the host names: refused with nothing changed, and the recording goes on."""
+    cache = U.make(1, 2, 1, 64, 32, "f16", 4, weighted=True)
+    cache.reserve([64])
+    x = U.rows(1, 1, 1, 64, 64, dtype="f16").to(U.DEVICE)
+    q = U.rows(2, 1, 2, 64, dtype="f16").to(U.DEVICE)
+    cache.append(x, x)
+    expected, out = cache.decode_attn(q), torch.zeros_like(q)
+    held = lambda: (dict(cache.free), [[list(i) for i in half] for half in cache.ids], list(cache.pages), cache.counts(), list(cache.cur))
+    before = held()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        for call in (lambda: cache.reserve([128]), lambda: cache.reserve([32], spare=True), lambda: cache.set_pages(0, [0, 1, 2]), lambda: cache.evict(32)):
+            with pytest.raises(binding.LogQuantError) as e:
+                call()
+            assert e.value.status == binding.LQ_ERR_STATE
+        cache.reserve([64])                                              # (takes none)
+        cache.decode_attn(q, out)
+    assert held() == before
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, expected)
+    cache.evict(32)
+    assert cache.counts() == [32]
