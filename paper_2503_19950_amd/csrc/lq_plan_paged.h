@@ -16,7 +16,7 @@ struct PlanPaged {
 // As for the 8-bit cache, whose unit of codes has half the bytes of a unit here.  rows: n tokens each.  What a step stages in LDS
 // (its queries, the new key and value) counts towards what a workgroup may have.
 // A weighted cache's logits stay in LDS where no item is split and the longest row's fit, so that the workgroup adds the weights
-// itself: 64 rows of up to 4096 tokens x 8 kv heads, 4 heads each: 101 us, through memory and a second launch 122 (94 without
+// itself: 64 rows of up to 4096 tokens x 8 kv heads, 4 heads each: 87 us, through memory and a second launch 107 (83 without
 // weights).  Workgroups of 4 wavefronts leave room for a second one on the compute unit.
 constexpr int LDS_OF_CU = 160 * 1024;
 inline bool plan_paged(const ShapePaged& s, int window, bool step, bool same, Row8* rows, int n_rows, PlanPaged* p) {

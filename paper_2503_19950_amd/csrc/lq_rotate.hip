@@ -5,8 +5,8 @@
 // lane's token and channels stay the same, so that its cosines and sines are in registers, computed once by the workgroup
 // together.  The other halves of a lane's pairs come from the lane that has them; all of a row is read before any of it is
 // written, so that a row may be written where it was read.
-// 32768 tokens x 40 heads, d = 128, bf16 (671 MB): 130 us (4 and 8 heads under way a lane: 132 and 138; without
-// the stores' way past the caches 139); a copy of as much takes 130.
+// 32768 tokens x 40 heads, d = 128, bf16 (671 MB): 128 us (4 and 8 heads under way a lane 2 and 8 more; without
+// the stores' way past the caches 139); a copy of as much takes 132.
 #include "lq_internal.h"
 #include "lq_paged.h"
 #include "lq_quant8.h"
