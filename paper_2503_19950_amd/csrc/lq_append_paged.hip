@@ -4,8 +4,8 @@
 // positions it computes the unit's cosines and sines once, into LDS.  Keys go over 16 bytes a lane, as they lie in a row of
 // the prompt; values as two channels of eight tokens a lane, whose halves are the pieces of the page.
 // 8 rows of 8192 tokens x 8 kv heads, d = 128 (537 MB): 104 us, with keys turned on their way 105 (5.1 TB/s, what a copy
-// reaches); rows of up to 8191 (270 MB): 60 and 61, of which some 8 us are workgroups that find their row at an end.
-// Stores past the caches: 121 and 68.
+// reaches); rows of up to 8191 (270 MB): 60 and 61; one row of 32768 (268 MB) 58, so the workgroups that find their
+// row at an end cost some 2 us (a grid without them, whose workgroups look for their row: 1 us less).  Stores past the caches: 121 and 68.
 #include "lq_internal.h"
 #include "lq_paged.h"
 #include "lq_quant8.h"
