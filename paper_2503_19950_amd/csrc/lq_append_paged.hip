@@ -99,7 +99,6 @@ __global__ void __launch_bounds__(64 * WAVES, TURN == HALVES_64 ? 3 : 1) append_
       if (x % 32 >= low && x % 32 < high)
         P.weights[((((int64_t)row.b * P.Hkv + head0 + x / 32) * P.max_pages) << P.log_p) + 32 * unit + x % 32] = 0.f;
   const int id = P.table[(int64_t)row.b * P.max_pages + (unit >> (P.log_p - 5))];
-  if (!is_page(id, P.n_pages)) return;
   // A lane computes the angles of one pair for every fourth token.  What it takes to compute them is loaded first (loads arrive in
   // order), then the first head's rows, which are under way meanwhile.
   const int pairs = P.rope.dims / 2;
@@ -146,6 +145,7 @@ __global__ void __launch_bounds__(64 * WAVES, TURN == HALVES_64 ? 3 : 1) append_
       if (lane < pairs) cs[(wave + j * WAVES) * PITCH + lane] = turn_of(freq, position[j], P.rope.factor);
     __syncthreads();
   }
+  if (!is_page(id, P.n_pages)) return;                                  // (loads do not wait for the table: 0 to 2 % by size)
   for (; h < head1; h += WAVES) {
     const int64_t off = unit_offset(id, P.Hkv, h, P.log_p, unit, D);
 #pragma unroll
