@@ -50,7 +50,8 @@ __device__ __forceinline__ u32x4 other_halves(__amdgpu_buffer_rsrc_t rs, int row
     }
   return y;
 }
-// Channels c0 .. c0+7 turned; y: other_halves; angle: that token's.  (The results of turn_pair, bit for bit.)
+// Channels c0 .. c0+7 turned; y: other_halves; angle: that token's, PITCH of them, of which dims / 2 have been computed and others are
+// read for channels that stay alone.  (The results of turn_pair, bit for bit.)
 template <bool BF16, int TURN>
 __device__ __forceinline__ u32x4 turned(int c0, u32x4 x, u32x4 y, int dims, const float2* angle) {
   if constexpr (TURN == NEIGHBOURS) {
@@ -63,11 +64,12 @@ __device__ __forceinline__ u32x4 turned(int c0, u32x4 x, u32x4 y, int dims, cons
     return x;
   }
   const int half = dims / 2;
+  const float2* of_piece = angle + (TURN == HALVES ? angle_of(c0, dims, 8) : c0 < half ? c0 : c0 - half);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int c = c0 + e, sh = 16 * (e & 1);
     const bool first = TURN == ODD ? c < half : c0 < half;
-    const float2 cs = TURN == ODD ? angle[first ? c : c - half] : (angle + (first ? c0 : c0 - half))[e];
+    const float2 cs = TURN == ODD ? angle[angle_of(c, dims, 1)] : of_piece[e];
     const float own = t2f<BF16>((uint16_t)(x[e / 2] >> sh)), other = t2f<BF16>((uint16_t)(y[e / 2] >> sh));
     const uint32_t z = f2t<BF16>(fmaf(own, cs.x, other * (first ? -cs.y : cs.y)));
     if (c < dims) x[e / 2] = (x[e / 2] & ~(0xFFFFu << sh)) | z << sh;

@@ -20,6 +20,13 @@ LQ8_HD int64_t unit_offset(int id, int Hkv, int h, int log_p, int unit, int d) {
   return ((((int64_t)id * Hkv + h) << log_p) + ((unit & ((1 << (log_p - 5)) - 1)) << 5)) * d;
 }
 
+// Where the angles of `wide` channels from c on begin among the dims / 2 of a token whose pairs are halves.  Channels that are not
+// turned have angles that are there, too.
+LQ8_HD int angle_of(int c, int dims, int wide) {
+  const int half = dims / 2, last = half - wide;
+  return c < half ? c : c - half < last ? c - half : last;
+}
+
 // Tokens seen .. n - 1 of a row get weight; the units that hold them, and those of one part of an item.
 LQ8_HD int first_seen(int n, int window) { return window > 0 && n > window ? n - window : 0; }
 struct PartPaged { int seen, pos, stop; };
