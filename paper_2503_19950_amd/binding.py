@@ -5,6 +5,7 @@ include/logquant.h.  PyTorch appears only as the owner of device memory and of
 the HIP stream; every step of the path runs in the library's kernels.  There is
 no fallback: if the shared library is missing, importing this module fails.
 """
+import collections
 import ctypes as C
 import os
 
@@ -879,23 +880,37 @@ class DeviceCachePaged:
         """Pages out of the pool for counts[b] tokens of every row (`spare`: for its next eviction).  LogQuantError
         (LQ_ERR_CAPACITY) if the pool or a row's table has too few, or (LQ_ERR_STATE) if any are to be taken while a graph is
         recorded; nothing is taken then."""
-        cfg = self.cfg
-        if len(counts) != cfg.B:
-            raise ValueError("reserve: expected %d counts" % cfg.B)
-        more = []
-        for b, count in enumerate(counts):
-            half = self.cur[b] ^ int(bool(spare))
-            need = -(-int(count) // cfg.page)
+        if len(counts) != self.cfg.B:
+            raise ValueError("reserve: expected %d counts" % self.cfg.B)
+        self._take("reserve", [(b, int(count)) for b, count in enumerate(counts) if count > 0], spare)
+
+    def _take(self, call, counts, spare):
+        """reserve for the rows of `counts`, [(row, tokens)].  Spare pages that an eviction left and that another row names as
+        well are given back first."""
+        cfg, uses = self.cfg, self.uses
+        halves = [self.cur[b] ^ int(bool(spare)) for b, _ in counts]
+        back = set()                                                     # rows that give back theirs
+        if spare and self.shared:
+            back = {b for (b, _), half in zip(counts, halves) if any(uses[i] > 1 for i in self.ids[half][b])}
+        more, total = [], 0
+        for (b, count), half in zip(counts, halves):
+            need = -(-count // cfg.page)
             if need > cfg.max_pages:
-                raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
-            need -= len(self.ids[half][b])
+                raise LogQuantError(LQ_ERR_CAPACITY, call)
+            need -= 0 if b in back else len(self.ids[half][b])
             if need > 0:
                 more.append((half, b, need))
-        if sum(need for _, _, need in more) > len(self.free):
-            raise LogQuantError(LQ_ERR_CAPACITY, "reserve")
-        if not more:
-            return
-        self._no_recording("reserve")
+                total += need
+        room = len(self.free)
+        if back:
+            named = collections.Counter(i for (b, _), half in zip(counts, halves) if b in back for i in self.ids[half][b])
+            room += sum(uses[i] == times for i, times in named.items())
+        if total > room:
+            raise LogQuantError(LQ_ERR_CAPACITY, call)
+        if more:
+            self._no_recording(call)
+        for b in back:
+            self.release(b, spare=True)
         names = []
         for half, b, need in more:
             ids = self.ids[half][b]
@@ -975,13 +990,18 @@ class DeviceCachePaged:
     def evict(self, keep, recent=0):
         """Rows with more than `keep` tokens (a number, or one for every row) keep the newest `recent` and the heaviest
         others, in pages that are taken from the pool if the row has too few spare ones.  The pages that it leaves are its
-        spare ones (`release(b, spare=True)` gives them back)."""
+        spare ones (`release(b, spare=True)` gives them back).  A call that is refused (counts, a pool without room, pages to
+        be taken while a graph is recorded) changes nothing."""
         keep = [int(keep)] * self.cfg.B if isinstance(keep, int) else [int(x) for x in keep]
         if len(keep) != self.cfg.B:
             raise ValueError("keep: expected %d counts" % self.cfg.B)
-        if any(n > x for n, x in zip(self.n, keep)):
-            for b, (n, x) in enumerate(zip(self.n, keep) if self.shared else ()):
-                if n > x and any(self.uses[i] > 1 for i in self.ids[self.cur[b] ^ 1][b]):   # left by an eviction, but another row's as well
-                    self.release(b, spare=True)
-            self.reserve([x if n > x else 0 for n, x in zip(self.n, keep)], spare=True)
+        recent = int(recent)
+        # what the call refuses is refused before pages are taken: with every row's count to keep it only checks
+        _on_device(self._index, _evict_paged, self._cfg, self._c, self.n, recent, self._ws)
+        lose = [(b, x) for b, (n, x) in enumerate(zip(self.n, keep)) if n > x]
+        if min(keep) < 0 or any(recent > x for _, x in lose):
+            raise LogQuantError(LQ_ERR_SHAPE, _evict_paged.__name__)
+        if not lose:
+            return
+        self._take("evict", lose, True)
         _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)

@@ -1,0 +1,73 @@
+"""Calls of the paged cache on the GPU that are refused, and what works behind them."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_19950_amd import binding
+from tests import gpu_util_paged as U
+
+pytestmark = pytest.mark.gpu
+
+
+def held(cache):
+    return (dict(cache.free), list(cache.uses), [[list(i) for i in half] for half in cache.ids], list(cache.pages), cache.shared,
+            cache.counts(), list(cache.cur), cache.table.tolist())
+
+
+def shared_prompt(d=64, dtype="f16"):
+    """Rows 0 and 1 read a prompt of 64 tokens; row 0 has been evicted from."""
+    cache = U.make(2, 2, 1, d, 32, dtype, 4, n_pages=9, weighted=True)
+    model = U.Model(cache, dtype)
+    K, V = U.rows(1, 2, 1, 64, d, dtype=dtype), U.rows(2, 2, 1, 64, d, dtype=dtype)
+    K[:], V[:] = K[:1], V[:1]
+    cache.reserve([64, 0])
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), [64, 0])
+    cache.set_pages(1, cache.ids[0][0])
+    cache.set_counts([64, 64])
+    model.append(K, V)
+    w = np.random.RandomState(1).rand(2, 1, 64).astype(np.float32)
+    cache.weights[0, :, :, :64] = torch.from_numpy(w).to(U.DEVICE)
+    model.w = [x.astype(np.float64) for x in w]
+    cache.evict([50, 64], 8)
+    model.evict([50, 64], 8)
+    return cache, model
+
+
+def test_a_refused_eviction_leaves_the_pages_of_a_shared_prompt():
+    """In a recording, with too many newest tokens, without room: nothing changes, and the next call goes on from there."""
+    cache, model = shared_prompt()
+    q = U.rows(3, 2, 2, 64, dtype="f16")
+    Q = q.to(U.DEVICE)
+    before, out = held(cache), torch.zeros_like(Q)
+    weights = cache.weights.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        with pytest.raises(binding.LogQuantError) as e:
+            cache.evict([40, 64], 8)
+        assert e.value.status == binding.LQ_ERR_STATE
+        cache.decode_attn(Q, out)
+    assert held(cache) == before
+    for kw, status in ((dict(keep=[40, 64], recent=41), binding.LQ_ERR_SHAPE), (dict(keep=[40, 64], recent=-1), binding.LQ_ERR_SHAPE)):
+        with pytest.raises(binding.LogQuantError) as e:
+            cache.evict(**kw)
+        assert e.value.status == status and held(cache) == before
+    taken = cache.free
+    cache.free = {}
+    with pytest.raises(binding.LogQuantError) as e:
+        cache.evict([40, 64], 8)
+    cache.free = taken
+    assert e.value.status == binding.LQ_ERR_CAPACITY and held(cache) == before
+    for _ in range(2):
+        cache.weights.copy_(weights)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        model.check_output(out, q)
+    cache.weights.copy_(weights)
+    pools = U.pools(cache)
+    cache.evict([40, 64], 8)
+    model.evict([40, 64], 8)
+    U.check_rows(cache, model, pools)
+    w = U.live_weights(cache)
+    assert all(np.array_equal(w[b, :, :cache.n[b]], model.w[b]) for b in range(2))
