@@ -858,7 +858,8 @@ class DeviceCachePaged:
 
     def set_pages(self, b, ids, spare=False):
         """The pages of row b's tokens, in order (`spare`: those that its next eviction moves to, which nothing else may
-        name).  Pages that were named there before, and by nothing else, go back to the pool."""
+        name).  Pages that were named there before, and by nothing else, go back to the pool.  A row's spare pages, those that
+        an eviction left among them, are refused unless some row still reads them."""
         self._no_recording("set_pages")
         ids = [int(i) for i in ids]
         if len(ids) > self.cfg.max_pages or any(not 0 <= i < self.cfg.n_pages for i in ids):
@@ -871,9 +872,10 @@ class DeviceCachePaged:
             if len(set(ids)) < len(ids) or any(self.uses[i] > (i in mine) for i in ids):
                 raise ValueError("set_pages: a spare page is one that nothing else names")
         else:
-            named = set(ids)
-            if any(i in named for row in range(self.cfg.B) for i in self.ids[self.cur[row] ^ 1][row]):
-                raise ValueError("set_pages: a row's spare page is not another's")
+            rows = range(self.cfg.B)
+            left = set(ids).intersection(i for row in rows for i in self.ids[self.cur[row] ^ 1][row])
+            if left and not left <= {i for row in rows for i in self.ids[self.cur[row]][row]}:
+                raise ValueError("set_pages: a row's spare page is not another's (release(row, spare=True) gives it back)")
         self._upload([self._name(half, b, ids, 0)])
 
     def reserve(self, counts, spare=False):

@@ -71,3 +71,14 @@ def test_a_refused_eviction_leaves_the_pages_of_a_shared_prompt():
     U.check_rows(cache, model, pools)
     w = U.live_weights(cache)
     assert all(np.array_equal(w[b, :, :cache.n[b]], model.w[b]) for b in range(2))
+
+
+def test_a_prompt_is_shared_on_after_one_of_its_readers_was_evicted_from():
+    cache, model = shared_prompt()
+    cache.set_pages(0, cache.ids[cache.cur[0]][0])                       # its own again: nothing changes
+    cache.release(0)
+    cache.set_pages(0, cache.ids[0][1])                                  # joins the prompt again, which row 1 reads
+    cache.set_counts([64, 64])
+    model.K[0], model.V[0] = model.K[1], model.V[1]
+    q = U.rows(3, 2, 2, 64, dtype="f16")
+    model.check_output(cache.decode_attn(q.to(U.DEVICE)), q)

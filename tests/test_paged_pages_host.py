@@ -176,3 +176,27 @@ def test_reserved_spare_pages_are_ones_that_the_eviction_takes(host):
     host.recording = False
     consistent(cache)
     assert cache.counts() == [40, 64, 0]
+
+
+def test_a_prompt_is_shared_on_after_one_of_its_readers_was_evicted_from(host):
+    cache, prompt = with_a_left_prompt()
+    cache.set_pages(2, prompt)                           # a new reader
+    cache.set_counts([60, 64, 64])
+    cache.set_pages(1, prompt + [cache.free.popitem()[0]])   # a reader names its pages again, and one more
+    consistent(cache)
+    assert [cache.uses[i] for i in prompt] == [3, 3]
+    cache.evict([40, 64, 64], 8)                         # row 0 moves elsewhere
+    consistent(cache)
+    assert not set(prompt) & set(cache.ids[cache.cur[0]][0]) and [cache.uses[i] for i in prompt] == [2, 2]
+
+
+def test_a_page_that_nobody_reads_any_more_is_not_named_before_it_is_given_back(host):
+    cache, prompt = with_a_left_prompt()
+    cache.release(1)
+    before = held(cache)
+    with pytest.raises(ValueError):
+        cache.set_pages(2, prompt)
+    assert held(cache) == before
+    cache.release(0, spare=True)
+    cache.set_pages(2, prompt)
+    consistent(cache)
