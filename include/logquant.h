@@ -521,7 +521,8 @@ lq_status logquant_workspace_init_paged(const lq_config_paged *cfg, void *worksp
  * logquant_append8.
  *   rope      : null, or the keys are turned on their way (v_new is not);
  *   positions : DEVICE [B][n_max] int32, with a rope; null: those behind the row's tokens,
- *               n[b], n[b]+1, .. (the right ones until a row has been evicted from).
+ *               n[b], n[b]+1, ..  A row that has been evicted from holds fewer tokens than
+ *               have come: from then on its positions are the caller's to count and pass.
  * New tokens of a weighted cache have weight 0.  LQ_ERR_CAPACITY if a row would pass its
  * pages[cur[b]][b] pages.  On success n[b] += n_new[b]; the caller may set n[b] back to
  * drop tokens. */
@@ -553,9 +554,10 @@ lq_status logquant_decode_attn_paged(const lq_config_paged *cfg, lq_cache_paged 
                                      const void *q, float softmax_scale, void *out, void *workspace, void *stream);
 
 /* One decode step: q and the new key of every row turned by rope (null: not) at
- * positions[b] (DEVICE [B]; null: n[b]), logquant_append_paged of that token, and
- * logquant_decode_attn_paged with that query over the cache including it, with the results
- * of the three calls (outputs and weights up to the order of fp32 sums).
+ * positions[b] (DEVICE [B]; null: n[b], as for logquant_append_paged), then
+ * logquant_append_paged of that token and logquant_decode_attn_paged with that query over
+ * the cache including it, with the results of the three calls (outputs and weights up to
+ * the order of fp32 sums).
  *   k_new, v_new : DEVICE [B][Hkv][1][d] T.  LQ_ERR_CAPACITY if a row has no room. */
 lq_status logquant_decode_step_paged(const lq_config_paged *cfg, lq_cache_paged *cache, const lq_rope *rope,
                                      const int32_t *positions, const lq_scores *scores, const void *k_new,

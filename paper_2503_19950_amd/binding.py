@@ -800,6 +800,7 @@ class DeviceCachePaged:
         self.ids = [[[] for _ in range(B)] for _ in range(2)]     # pages that the table names, by half and row
         self.free, self.uses = dict.fromkeys(range(cfg.n_pages - 1, -1, -1)), [0] * cfg.n_pages
         self.shared = 0                                           # pages that are named more than once
+        self.gaps = set()                                         # halves of rows, half * B + row, that were evicted into
         self.c = lq_cache_paged(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.table.data_ptr(),
                                 self.weights.data_ptr() if cfg.weighted else None, *(C.cast(x, _I32P) for x in (self.n, self.cur, self.pages)),
                                 self.seq_state.data_ptr())
@@ -819,6 +820,7 @@ class DeviceCachePaged:
         other.shared = self.shared
         other.pages[:] = list(self.pages)
         other.set_counts(self.counts(), list(self.cur))
+        other.gaps = set(self.gaps)
         return other
 
     # ---- pages
@@ -841,6 +843,8 @@ class DeviceCachePaged:
                 self.shared -= 1
         row = half * self.cfg.B + b
         self.pages[row] = len(ids)
+        if not ids:
+            self.gaps.discard(row)
         at = row * self.cfg.max_pages
         return range(at + first, at + len(ids)), ids[first:]
 
@@ -932,13 +936,16 @@ class DeviceCachePaged:
         return list(self.n)
 
     def set_counts(self, counts, cur=None):
-        """Set the host-side counts (the device buffers are left as they are), and, where given, which half is every row's."""
+        """Set the host-side counts (the device buffers are left as they are), and, where given, which half is every row's.  A
+        row of 0 tokens begins anew."""
         self.n[:] = counts
         if cur is not None:
             self.cur[:] = cur
+        if self.gaps:
+            self.gaps.difference_update([self.cur[b] * self.cfg.B + b for b, n in enumerate(self.n) if not n])
 
     # ---- calls
-    def _turn(self, rope, positions, n):
+    def _turn(self, rope, positions, n, n_new=None):
         if rope is None:
             if positions is not None:
                 raise ValueError("positions without a rope")
@@ -946,6 +953,10 @@ class DeviceCachePaged:
         if rope.index != self._index:
             raise ValueError("rope: expected it on %s" % self.device)
         if positions is None:
+            if self.gaps:
+                for b in range(self.cfg.B):
+                    if self.cur[b] * self.cfg.B + b in self.gaps and (n_new is None or n_new[b]):
+                        raise ValueError("positions: row %d was evicted from, its tokens' places are not their positions" % b)
             return rope._c, None
         shape = (self.cfg.B,) if n == 1 and positions.dim() == 1 else (self.cfg.B, n)
         return rope._c, _tensor("positions", positions, shape, torch.int32, self.device)
@@ -958,14 +969,15 @@ class DeviceCachePaged:
 
     def append(self, k_new, v_new, n_new=None, rope=None, positions=None):
         """k_new, v_new: [B][Hkv][n][d]; n_new: tokens that each row takes of them, 0..n (None: all).  With a rope, keys are
-        turned by positions ([B][n] int32; None: the places of the tokens)."""
+        turned by positions ([B][n] int32; None: the places of the tokens, refused for a row that was evicted from and takes
+        any)."""
         c = self.cfg
         n = k_new.shape[2] if k_new.dim() == 4 else 1
         shape = self._token if n == 1 else torch.Size((c.B, c.Hkv, n, c.d))
         k, v = _tensor("k_new", k_new, shape, self.dtype, self.device), _tensor("v_new", v_new, shape, self.dtype, self.device)
         if n_new is not None and len(n_new) != c.B:
             raise ValueError("n_new: expected %d counts" % c.B)
-        turn, at = self._turn(rope, positions, n)
+        turn, at = self._turn(rope, positions, n, n_new)
         _on_device(self._index, _append_paged, self._cfg, self._c, turn, at, k, v, _i32(n_new), n)
 
     def decode_attn(self, q, out=None, softmax_scale=0.0, softcap=0.0, window=0, slopes=None):
@@ -979,7 +991,7 @@ class DeviceCachePaged:
 
     def decode_step(self, k_new, v_new, q, out=None, softmax_scale=0.0, rope=None, positions=None, softcap=0.0, window=0, slopes=None):
         """Append one token per row ([B][Hkv][1][d]) and attend; with a rope, its key and the query are turned by positions
-        ([B] int32; None: the places of the tokens)."""
+        ([B] int32; None: the places of the tokens, refused after an eviction)."""
         if out is None:
             out = torch.empty_like(q)
         turn, at = self._turn(rope, positions, 1)
@@ -1007,3 +1019,4 @@ class DeviceCachePaged:
             return
         self._take("evict", lose, True)
         _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)
+        self.gaps.update(self.cur[b] * self.cfg.B + b for b, _ in lose)

@@ -82,3 +82,25 @@ def test_a_prompt_is_shared_on_after_one_of_its_readers_was_evicted_from():
     model.K[0], model.V[0] = model.K[1], model.V[1]
     q = U.rows(3, 2, 2, 64, dtype="f16")
     model.check_output(cache.decode_attn(q.to(U.DEVICE)), q)
+
+
+def test_tokens_behind_an_eviction_are_turned_by_positions_alone():
+    cache, model = shared_prompt()
+    cache.set_pages(1, cache.ids[0][1] + [cache.free.popitem()[0]])
+    rope = binding.Rope(binding.logquant_rope_frequencies(64), device=U.DEVICE)
+    K, V, q = U.rows(4, 2, 1, 1, 64, dtype="f16"), U.rows(5, 2, 1, 1, 64, dtype="f16"), U.rows(6, 2, 2, 64, dtype="f16")
+    before, pools = held(cache), U.pools(cache)
+    with pytest.raises(ValueError):
+        cache.decode_step(K.to(U.DEVICE), V.to(U.DEVICE), q.to(U.DEVICE), rope=rope)
+    with pytest.raises(ValueError):
+        cache.append(K.to(U.DEVICE), V.to(U.DEVICE), rope=rope)
+    assert held(cache) == before
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), [0, 1], rope=rope)      # the other row's places are its positions
+    model.append(binding.rotate(rope, torch.full((2,), 64, dtype=torch.int32, device=U.DEVICE), k=K.to(U.DEVICE))[1].cpu(), V, [0, 1])
+    U.check_rows(cache, model, pools)
+    at = torch.tensor([64, 65], dtype=torch.int32, device=U.DEVICE)
+    tq, tk = (x.cpu() for x in binding.rotate(rope, at, q[:, :, None].contiguous().to(U.DEVICE), K.to(U.DEVICE)))
+    out = cache.decode_step(K.to(U.DEVICE), V.to(U.DEVICE), q.to(U.DEVICE), rope=rope, positions=at)
+    model.append(tk, V)
+    U.check_rows(cache, model, pools)
+    model.check_output(out, tq[:, :, 0])

@@ -200,3 +200,39 @@ def test_a_page_that_nobody_reads_any_more_is_not_named_before_it_is_given_back(
     cache.release(0, spare=True)
     cache.set_pages(2, prompt)
     consistent(cache)
+
+
+def test_places_are_no_positions_after_an_eviction(host):
+    """A row that was evicted from holds fewer tokens than have come: keys are not turned by places any more."""
+    cache = make()
+    rope = B.Rope([1.0, 0.5], device="cpu")
+    turn = lambda **kw: cache._turn(rope, None, 1, **kw)  # noqa: E731
+    cache.reserve([96, 96, 96])
+    cache.set_counts([64, 32, 0])
+    assert turn()[1] is None
+    cache.evict(40, 8)                                   # row 0
+    with pytest.raises(ValueError):
+        turn()
+    with pytest.raises(ValueError):
+        turn(n_new=[1, 1, 1])
+    turn(n_new=[0, 1, 1])                                # it takes none
+    assert cache._turn(None, None, 1) == (None, None) and cache.counts() == [40, 32, 0]
+    other = cache.clone()
+    with pytest.raises(ValueError):
+        other._turn(rope, None, 1)
+    cache.set_counts([64, 32, 0], [0, 0, 0])             # back to the tokens that were all there
+    turn()
+    cache.set_counts([39, 32, 0], [1, 0, 0])             # and on again, a token dropped
+    with pytest.raises(ValueError):
+        turn()
+    cache.set_counts([0, 32, 0])                         # begins anew
+    turn()
+    other.release(0)
+    other._turn(rope, None, 1)
+    other.release(1)
+    other.set_counts([0, 0, 0])
+    assert not other.gaps
+    cache.set_counts([64, 32, 0], [0, 0, 0])
+    cache.evict([0, 32, 0])                              # an empty row whose next token is not the first
+    with pytest.raises(ValueError):
+        turn()
