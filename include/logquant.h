@@ -478,7 +478,8 @@ lq_status logquant_rotate(const lq_rope *rope, int32_t B, int32_t L, int32_t Hq,
  * Slots at and behind a row's length are neither written nor do they influence a result.
  * A page that several rows name must be full of tokens that they share: a call that
  * writes to it for two of them leaves either's.  An entry of the table that is outside
- * 0 .. n_pages-1 is no page: its tokens get no attention and nothing is stored for them.
+ * 0 .. n_pages-1 is no page: its tokens get no attention and nothing is stored for them
+ * (until an eviction gives them a page, see there).
  *
  * n, cur and pages are HOST arrays, owned by the caller and, n and cur, updated by the
  * calls; seq_state, streams, graphs (a recorded call keeps its counts, and reads table and
@@ -571,6 +572,11 @@ lq_status logquant_decode_step_paged(const lq_config_paged *cfg, lq_cache_paged 
  * that the other half of the table names for row b, their weights to the other half of
  * weights, and that half becomes the row's: n[b] = keep[b], cur[b] flips.  The pages of the
  * half that was are the caller's again.  Other rows stay as they are.
+ * A token without a page gets no weight, so it goes before those that have some.  Where it
+ * stays (among the newest, or because too few others are there) its new place holds zeros,
+ * and from then on it is a token like any other, with a key and a value of zeros: it takes
+ * part in the softmax with a score of 0 before cap and bias, and gets weight.  A caller
+ * whose rows have such entries keeps no more tokens than those that have pages.
  * Weights are compared as fp32 numbers and must not be NaN.  New pages must not be among
  * those that a row reads.  LQ_ERR_STATE unless `weighted`; LQ_ERR_SHAPE for a negative keep,
  * recent < 0, or recent > keep[b] of a row that loses tokens; LQ_ERR_CAPACITY if

@@ -301,6 +301,7 @@ __global__ void __launch_bounds__(256) count_kernel(const EvictParams P, const R
 }
 
 // Rows to their new places: a wavefront a unit of 32 slots.  grid (units / 4, Hkv, rows)
+// A token that had no page becomes one of zeros: its new slot lies among others' in a page, and attention knows pages, not slots.
 // Keys are pieces of 16 bytes of a token, gathered.  A piece of values holds eight tokens: units that the tokens come from are read
 // whole, 16 bytes a lane, and what stays of them is put in its place in LDS, two bytes at a time.  Where the tokens of a unit come
 // from more than DENSE others (few stay of many), they are gathered from memory two bytes at a time instead: 8 rows of 16384 tokens x 8

@@ -104,3 +104,36 @@ def test_tokens_behind_an_eviction_are_turned_by_positions_alone():
     model.append(tk, V)
     U.check_rows(cache, model, pools)
     model.check_output(out, tq[:, :, 0])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_tokens_without_a_page_are_tokens_of_zeros_behind_an_eviction(dtype):
+    """Before it they get no attention and no weight; those that stay take part in the softmax as a key and a value of zeros."""
+    Hkv, d, page, lengths = 2, 64, 32, [96, 70]
+    cache = U.make(2, 4, Hkv, d, page, dtype, 4, weighted=True)
+    cache.reserve(lengths)
+    K, V = U.rows(1, 2, Hkv, 96, d, dtype=dtype), U.rows(2, 2, Hkv, 96, d, dtype=dtype)
+    cache.append(K.to(U.DEVICE), V.to(U.DEVICE), lengths)
+    cache.table[0, 0, 1] = -1                                            # row 0: 32 of its 96 tokens
+    q = U.rows(3, 2, 4, d, dtype=dtype)
+    seen = U.Model(cache, dtype)                                         # what attends: row 0 without them
+    seen.append(K, V, lengths)
+    seen.K[0], seen.V[0] = (np.delete(x[0], np.s_[32:64], 1) for x in (seen.K, seen.V))
+    seen.check_output(cache.decode_attn(q.to(U.DEVICE)), q)
+    w = U.live_weights(cache)
+    assert (w[0, :, 32:64] == 0).all() and (w[0, :, :32] > 0).all() and (w[0, :, 64:96] > 0).all()
+    model = U.Model(cache, dtype)
+    model.append(K, V, lengths)
+    model.K[0][:, 32:64] = model.V[0][:, 32:64] = 0
+    model.w = [w[b, :, :n].copy() for b, n in enumerate(lengths)]
+    # 64 tokens have a page: of 60 that stay none is without one, of 70 six are
+    for keep in (60, 70):
+        one, two = cache.clone(), U.Model(cache, dtype)
+        one.table[0, 0, 1] = -1
+        two.K, two.V, two.w = ([x.copy() for x in t] for t in (model.K, model.V, model.w))
+        before = U.pools(one)
+        one.evict([keep, 70], 8)
+        two.evict([keep, 70], 8)
+        assert all((two.K[0][h] == 0).all(-1).sum() == max(0, keep - 64) for h in range(Hkv))
+        U.check_rows(one, two, before)
+        two.check_output(one.decode_attn(q.to(U.DEVICE)), q, weights=U.live_weights(one))
