@@ -350,8 +350,8 @@ hipError_t attn_paged(const ShapePaged& s, const AttnPagedParams& p, const Rows8
   auto with_type = [&](auto bf16) {
     const std::integral_constant<int, 1> one;
     if (plan.hb > 16) return with(bf16, std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-    if constexpr (MODE == ROWS_LISTED)                                  // (no plan has 16 for rows that are alike)
-      if (plan.waves == 16) return with(bf16, std::integral_constant<int, 16>{}, one);
+    if constexpr (MODE == ROWS_LISTED)                                  // (no plan has 16 for rows that are alike, or for larger heads)
+      if (plan.waves == 16) return go(attn_paged_kernel<decltype(bf16)::value, 64, 16, 1, MODE, STEP, MORE>);
     if (plan.waves == 8) return with(bf16, std::integral_constant<int, 8>{}, one);
     with(bf16, std::integral_constant<int, 4>{}, one);
   };
