@@ -56,10 +56,11 @@ static lq_status make_rope(const lq_rope* rope, int d, const int32_t* positions,
 
 static lq_status make_scores(const lq_scores* scores, const ShapePaged& s, float softmax_scale, ScoresArg* out) {
   const float log2e = 1.44269504088896340736f;
+  if (!isfinite(softmax_scale)) return LQ_ERR_SHAPE;
   if (!(softmax_scale > 0.f)) softmax_scale = 1.0f / sqrtf((float)s.d);
   *out = ScoresArg{softmax_scale * log2e, 0.f, 0, nullptr};
   if (scores) {
-    if (scores->window < 0 || isnan(scores->softcap) || !aligned4(scores->slopes)) return LQ_ERR_SHAPE;
+    if (scores->window < 0 || !isfinite(scores->softcap) || !aligned4(scores->slopes)) return LQ_ERR_SHAPE;
     out->window = scores->window;
     out->slopes = scores->slopes;
     if (scores->softcap > 0.f) {
