@@ -5,6 +5,7 @@ include/logquant.h.  PyTorch appears only as the owner of device memory and of
 the HIP stream; every step of the path runs in the library's kernels.  There is
 no fallback: if the shared library is missing, importing this module fails.
 """
+import array
 import collections
 import ctypes as C
 import os
@@ -281,10 +282,13 @@ def logquant_decode_plan(cfg, n_fp, n_q):
 
 
 def _i32(values):
-    """Host int32 array (or null) from a Python sequence."""
+    """Host int32 array (or null) from a Python sequence.  (ctypes by itself would take numbers modulo 2^32.)"""
     if values is None:
         return None
-    return (C.c_int32 * len(values))(*[int(x) for x in values])
+    try:
+        return (C.c_int32 * len(values)).from_buffer(array.array("i", map(int, values)) or bytearray(4))
+    except OverflowError:
+        raise ValueError("expected 32-bit numbers") from None
 
 
 def logquant_seq_state_bytes(cfg):
@@ -781,6 +785,7 @@ class DeviceCachePaged:
     goes to the current stream of the cache's device, whichever device is current."""
 
     BUFFERS = ("k_pages", "v_pages", "table", "weights")
+    INT_MAX = 2 ** 31 - 1                                         # more tokens than any row can have
 
     def __init__(self, cfg, device="cuda:0", poison=False):
         self.cfg = cfg
@@ -938,6 +943,9 @@ class DeviceCachePaged:
     def set_counts(self, counts, cur=None):
         """Set the host-side counts (the device buffers are left as they are), and, where given, which half is every row's.  A
         row of 0 tokens begins anew."""
+        counts, cur = _i32(counts), _i32(cur)
+        if len(counts) != self.cfg.B or (cur is not None and len(cur) != self.cfg.B):
+            raise ValueError("set_counts: expected %d of each" % self.cfg.B)
         self.n[:] = counts
         if cur is not None:
             self.cur[:] = cur
@@ -965,7 +973,7 @@ class DeviceCachePaged:
         if not softcap and not window and slopes is None:
             return None
         at = None if slopes is None else _tensor("slopes", slopes, (self.cfg.Hq,), torch.float32, self.device)
-        return C.byref(lq_scores(softcap, window, at))
+        return C.byref(lq_scores(softcap, max(-1, min(window, self.INT_MAX)), at))
 
     def append(self, k_new, v_new, n_new=None, rope=None, positions=None):
         """k_new, v_new: [B][Hkv][n][d]; n_new: tokens that each row takes of them, 0..n (None: all).  With a rope, keys are
@@ -1011,12 +1019,12 @@ class DeviceCachePaged:
             raise ValueError("keep: expected %d counts" % self.cfg.B)
         recent = int(recent)
         # what the call refuses is refused before pages are taken: with every row's count to keep it only checks
-        _on_device(self._index, _evict_paged, self._cfg, self._c, self.n, recent, self._ws)
+        _on_device(self._index, _evict_paged, self._cfg, self._c, self.n, max(-1, min(recent, self.INT_MAX)), self._ws)
         lose = [(b, x) for b, (n, x) in enumerate(zip(self.n, keep)) if n > x]
         if min(keep) < 0 or any(recent > x for _, x in lose):
             raise LogQuantError(LQ_ERR_SHAPE, _evict_paged.__name__)
         if not lose:
             return
         self._take("evict", lose, True)
-        _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)
+        _on_device(self._index, _evict_paged, self._cfg, self._c, _i32([min(n, x) for n, x in zip(self.n, keep)]), recent, self._ws)
         self.gaps.update(self.cur[b] * self.cfg.B + b for b, _ in lose)

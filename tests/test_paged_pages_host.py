@@ -236,3 +236,32 @@ def test_places_are_no_positions_after_an_eviction(host):
     cache.evict([0, 32, 0])                              # an empty row whose next token is not the first
     with pytest.raises(ValueError):
         turn()
+
+
+FAR = 2 ** 32                                            # what 32 bits would make 0 of
+
+
+def test_numbers_beyond_32_bits_are_not_taken_modulo(host):
+    cache = make()
+    cache.reserve([64, 32, 0])
+    cache.set_counts([64, 32, 0])
+    before = held(cache)
+    cache.evict(FAR)                                     # nobody has more
+    cache.evict([FAR + 8, 2 ** 63, FAR], FAR + 4)
+    assert held(cache) == before
+    for kw in (dict(keep=40, recent=FAR), dict(keep=40, recent=FAR + 8), dict(keep=40, recent=-FAR), dict(keep=8 - FAR), dict(keep=[FAR + 40, 8 - FAR, 0])):
+        with pytest.raises(B.LogQuantError) as e:
+            cache.evict(**kw)
+        assert e.value.status == B.LQ_ERR_SHAPE and held(cache) == before
+    for counts, cur in (([FAR + 5, 0, 0], None), ([0, -FAR, 0], None), ([5, 0, 0], [FAR, 0, 0]), ([5, 0], None), ([5, 0, 0], [1])):
+        with pytest.raises(ValueError):
+            cache.set_counts(counts, cur)
+        assert held(cache) == before
+    cache.evict([40, FAR, FAR + 1], 8)
+    assert cache.counts() == [40, 32, 0] and list(cache.cur) == [1, 0, 0]
+    assert cache._how(0.0, FAR, None)._obj.window == 2 ** 31 - 1 and cache._how(0.0, -FAR, None)._obj.window == -1
+    assert cache._how(0.0, 7, None)._obj.window == 7
+    for values in ([FAR], [0, -FAR - 1], [2 ** 31]):
+        with pytest.raises(ValueError):
+            B._i32(values)
+    assert list(B._i32([2 ** 31 - 1, -2 ** 31, True])) == [2 ** 31 - 1, -2 ** 31, 1] and B._i32(None) is None and len(B._i32([])) == 0
