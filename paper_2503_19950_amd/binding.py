@@ -853,6 +853,12 @@ class DeviceCachePaged:
         at = row * self.cfg.max_pages
         return range(at + first, at + len(ids)), ids[first:]
 
+    def _half(self, call, b, spare):
+        """Which half of the table a row's pages, or its spare ones, are in."""
+        if not 0 <= b < self.cfg.B:
+            raise ValueError("%s: expected a row in 0 .. %d" % (call, self.cfg.B - 1))
+        return self.cur[b] ^ int(bool(spare))
+
     def _no_recording(self, call):
         """Pages are named from the host, which a graph cannot record."""
         with torch.cuda.device(self.device):
@@ -873,7 +879,7 @@ class DeviceCachePaged:
         ids = [int(i) for i in ids]
         if len(ids) > self.cfg.max_pages or any(not 0 <= i < self.cfg.n_pages for i in ids):
             raise ValueError("set_pages: expected up to %d pages in 0 .. %d" % (self.cfg.max_pages, self.cfg.n_pages - 1))
-        half = self.cur[b] ^ int(bool(spare))
+        half = self._half("set_pages", b, spare)
         if not spare and len(ids) * self.cfg.page < self.n[b]:
             raise ValueError("set_pages: row %d holds %d tokens" % (b, self.n[b]))
         if spare:
@@ -931,9 +937,9 @@ class DeviceCachePaged:
     def release(self, b, spare=False):
         """Row b gives its pages back and is empty (`spare`: gives back those that it has for its next eviction, or had
         before its last)."""
+        half = self._half("release", b, spare)
         if not spare:
             self.n[b] = 0
-        half = self.cur[b] ^ int(bool(spare))
         self._name(half, b, [], 0)
 
     # ---- counts

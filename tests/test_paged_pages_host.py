@@ -265,3 +265,15 @@ def test_numbers_beyond_32_bits_are_not_taken_modulo(host):
         with pytest.raises(ValueError):
             B._i32(values)
     assert list(B._i32([2 ** 31 - 1, -2 ** 31, True])) == [2 ** 31 - 1, -2 ** 31, 1] and B._i32(None) is None and len(B._i32([])) == 0
+
+
+@pytest.mark.parametrize("row", [-1, -3, 3, 2 ** 31])
+def test_rows_that_the_cache_does_not_have(host, row):
+    cache = with_a_left_prompt()[0]
+    before = held(cache)
+    for spare in (False, True):
+        with pytest.raises(ValueError):
+            cache.set_pages(row, [cache.cfg.n_pages - 1], spare=spare)
+        with pytest.raises(ValueError):
+            cache.release(row, spare=spare)
+    assert held(cache) == before
