@@ -429,8 +429,10 @@ lq_status logquant_decode_step8(const lq_config8 *cfg, lq_cache8 *cache, const v
  * row at position p turns by the angle a = p * freq[i]:
  *   (x0, x1) -> factor * (x0 cos a - x1 sin a, x1 cos a + x0 sin a)
  * the other channels stay.  Pairs are channels (i, i + dims/2), or (2i, 2i+1) with
- * `interleaved`.  Angles are reduced in fp64, so far positions are as exact as near ones;
- * a result is computed in fp32 and rounded to T once.  A negative position turns back. */
+ * `interleaved`.  Angles are reduced in fp64 and go on in fp32 as less than half a turn: an
+ * angle is off by 2^-26 turns and 3 * 2^-53 of itself, which is more from about 2^28 radians
+ * on (2^31 radians: 2^-23 turns).  A result is computed in fp32 and rounded to T once.  A
+ * negative position turns back. */
 typedef struct {
   int32_t dims;          /* rotated channels, even, 2 .. d                               */
   int32_t interleaved;   /* 0: pairs (i, i + dims/2); 1: pairs (2i, 2i+1)                */
@@ -547,6 +549,8 @@ typedef struct {
  * over the tokens that row b holds; zeros for an empty row (or one without a page).
  * Weighted: weights[b][h][t] += the sum, over the query heads of kv head h, of the
  * probabilities of t.
+ * A probability enters the output to 2^-22 of itself or, in an fp16 cache, 2^-35 of the
+ * largest of its row and head, whichever is more.
  * Finite scores within fp32.  q, out, softmax_scale, workspace: as for
  * logquant_decode_attn8 (sizes from logquant_sizes_paged, prepared with
  * logquant_workspace_init_paged).  LQ_ERR_SHAPE for a negative window, or a softcap or

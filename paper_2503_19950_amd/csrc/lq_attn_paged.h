@@ -5,8 +5,9 @@
 // O^T = V^T P^T by matrix instructions of 16 x 16 x 32, up to 16 query heads of a kv head as the columns, a lane's four tokens
 // of a head being the elements that it owes to P^T.  Operands of keys and values are read from their pages as they lie, 16
 // bytes a lane; a unit of 32 tokens never crosses a page, and its page is looked up by a scalar load one unit ahead.
-// Probabilities are two operands of fp16 or three of bf16, what each rounding leaves going to the next, so that no rounding of
-// them is left (2^-22 or 2^-24 of each).
+// Probabilities are two operands of fp16 or three of bf16, what each rounding leaves going to the next, so that 2^-22 or 2^-24 of
+// each is left of their roundings; of fp16 ones, whose second operand is subnormal for a probability below 2^-3, at least 2^-25, where
+// the largest stands at 2^10 or more (BIAS): 2^-35 of it.  What is smaller adds to the sum (and to weights), not to the output.
 #pragma once
 #include <type_traits>
 
