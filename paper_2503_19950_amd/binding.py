@@ -5,10 +5,10 @@ include/logquant.h.  PyTorch appears only as the owner of device memory and of
 the HIP stream; every step of the path runs in the library's kernels.  There is
 no fallback: if the shared library is missing, importing this module fails.
 """
-import array
 import collections
 import ctypes as C
 import os
+from array import array
 
 # PyTorch ships its own HIP runtime.  It has to be in the process before the library
 # is loaded so that the library binds to that same runtime (matched by soname); two
@@ -286,7 +286,8 @@ def _i32(values):
     if values is None:
         return None
     try:
-        return (C.c_int32 * len(values)).from_buffer(array.array("i", map(int, values)) or bytearray(4))
+        values = array("i", map(int, values))
+        return (C.c_int32 * len(values)).from_buffer(values or bytearray(4))
     except OverflowError:
         raise ValueError("expected 32-bit numbers") from None
 
@@ -802,6 +803,7 @@ class DeviceCachePaged:
         self.weights = buf(self.sizes.weights).view(torch.float32).view(2, B, cfg.Hkv, -1) if cfg.weighted else None
         self.seq_state, self.workspace = buf(self.sizes.seq_state), buf(self.sizes.workspace)
         self.n, self.cur, self.pages = (C.c_int32 * B)(), (C.c_int32 * B)(), (C.c_int32 * (2 * B))()
+        self._at_n, self._at_cur = (memoryview(x).cast("B").cast("i") for x in (self.n, self.cur))
         self.ids = [[[] for _ in range(B)] for _ in range(2)]     # pages that the table names, by half and row
         self.free, self.uses = dict.fromkeys(range(cfg.n_pages - 1, -1, -1)), [0] * cfg.n_pages
         self.shared = 0                                           # pages that are named more than once
@@ -904,23 +906,25 @@ class DeviceCachePaged:
     def _take(self, call, counts, spare):
         """reserve for the rows of `counts`, [(row, tokens)].  Spare pages that an eviction left and that another row names as
         well are given back first."""
-        cfg, uses = self.cfg, self.uses
-        halves = [self.cur[b] ^ int(bool(spare)) for b, _ in counts]
-        back = set()                                                     # rows that give back theirs
-        if spare and self.shared:
-            back = {b for (b, _), half in zip(counts, halves) if any(uses[i] > 1 for i in self.ids[half][b])}
-        more, total = [], 0
-        for (b, count), half in zip(counts, halves):
-            need = -(-count // cfg.page)
-            if need > cfg.max_pages:
+        page, most, uses = self.cfg.page, self.cfg.max_pages, self.uses
+        cur, other = self.cur[:], int(bool(spare))
+        back, more, total = {}, [], 0                                    # back: spare pages that are given back, by row
+        for b, count in counts:
+            half = cur[b] ^ other
+            ids = self.ids[half][b]
+            need = -(-count // page)
+            if need > most:
                 raise LogQuantError(LQ_ERR_CAPACITY, call)
-            need -= 0 if b in back else len(self.ids[half][b])
+            if spare and self.shared and any(uses[i] > 1 for i in ids):
+                back[b] = ids
+            else:
+                need -= len(ids)
             if need > 0:
                 more.append((half, b, need))
                 total += need
         room = len(self.free)
         if back:
-            named = collections.Counter(i for (b, _), half in zip(counts, halves) if b in back for i in self.ids[half][b])
+            named = collections.Counter(i for ids in back.values() for i in ids)
             room += sum(uses[i] == times for i, times in named.items())
         if total > room:
             raise LogQuantError(LQ_ERR_CAPACITY, call)
@@ -949,12 +953,16 @@ class DeviceCachePaged:
     def set_counts(self, counts, cur=None):
         """Set the host-side counts (the device buffers are left as they are), and, where given, which half is every row's.  A
         row of 0 tokens begins anew."""
-        counts, cur = _i32(counts), _i32(cur)
-        if len(counts) != self.cfg.B or (cur is not None and len(cur) != self.cfg.B):
-            raise ValueError("set_counts: expected %d of each" % self.cfg.B)
-        self.n[:] = counts
-        if cur is not None:
-            self.cur[:] = cur
+        try:                                                      # (ctypes by itself would take numbers modulo 2^32)
+            counts = array("i", counts)
+            if cur is not None:
+                cur = array("i", cur)
+                if len(counts) != self.cfg.B:
+                    raise ValueError("set_counts: expected %d counts" % self.cfg.B)
+                self._at_cur[:] = cur
+            self._at_n[:] = counts
+        except OverflowError:
+            raise ValueError("set_counts: expected 32-bit numbers") from None
         if self.gaps:
             self.gaps.difference_update([self.cur[b] * self.cfg.B + b for b, n in enumerate(self.n) if not n])
 
@@ -1020,17 +1028,21 @@ class DeviceCachePaged:
         others, in pages that are taken from the pool if the row has too few spare ones.  The pages that it leaves are its
         spare ones (`release(b, spare=True)` gives them back).  A call that is refused (counts, a pool without room, pages to
         be taken while a graph is recorded) changes nothing."""
-        keep = [int(keep)] * self.cfg.B if isinstance(keep, int) else [int(x) for x in keep]
-        if len(keep) != self.cfg.B:
-            raise ValueError("keep: expected %d counts" % self.cfg.B)
+        B, n = self.cfg.B, self.n[:]
+        keep = [int(keep)] * B if isinstance(keep, int) else [int(x) for x in keep]
+        if len(keep) != B:
+            raise ValueError("keep: expected %d counts" % B)
         recent = int(recent)
         # what the call refuses is refused before pages are taken: with every row's count to keep it only checks
         _on_device(self._index, _evict_paged, self._cfg, self._c, self.n, max(-1, min(recent, self.INT_MAX)), self._ws)
-        lose = [(b, x) for b, (n, x) in enumerate(zip(self.n, keep)) if n > x]
-        if min(keep) < 0 or any(recent > x for _, x in lose):
+        if max(keep) > self.INT_MAX:
+            keep = [min(x, self.INT_MAX) for x in keep]
+        lose = [(b, x) for b, x in enumerate(keep) if n[b] > x]
+        if min(keep) < 0 or any([recent > x for _, x in lose]):
             raise LogQuantError(LQ_ERR_SHAPE, _evict_paged.__name__)
         if not lose:
             return
         self._take("evict", lose, True)
-        _on_device(self._index, _evict_paged, self._cfg, self._c, _i32([min(n, x) for n, x in zip(self.n, keep)]), recent, self._ws)
-        self.gaps.update(self.cur[b] * self.cfg.B + b for b, _ in lose)
+        _on_device(self._index, _evict_paged, self._cfg, self._c, _i32(keep), recent, self._ws)
+        cur = self.cur[:]
+        self.gaps.update([cur[b] * B + b for b, _ in lose])
