@@ -580,7 +580,8 @@ lq_status logquant_decode_step_paged(const lq_config_paged *cfg, lq_cache_paged 
  * stays (among the newest, or because too few others are there) its new place holds zeros,
  * and from then on it is a token like any other, with a key and a value of zeros: it takes
  * part in the softmax with a score of 0 before cap and bias, and gets weight.  A caller
- * whose rows have such entries keeps no more tokens than those that have pages.
+ * with such entries who does not want that has pages for the newest `recent`, and keeps no
+ * more tokens than have pages.
  * Weights are compared as fp32 numbers and must not be NaN.  New pages must not be among
  * those that a row reads.  LQ_ERR_STATE unless `weighted`; LQ_ERR_SHAPE for a negative keep,
  * recent < 0, or recent > keep[b] of a row that loses tokens; LQ_ERR_CAPACITY if
